@@ -137,7 +137,7 @@ def _quantise(x):
     """codes (whole numbers 0 .. 15, as x) and scale bytes (one for 32 values) of float rows [.., d]"""
     y = x.unflatten(-1, (-1, 32))
     m, e = torch.frexp(y.abs().amax(-1))
-    e = (e - 3 + (m > 0.875).int()).clamp(min=-100)              # the largest magnitude is at most 7 steps of 2^e
+    e = (e - 3 + (m > 0.875).int()).clamp(-100, 125)             # the largest magnitude is at most 7 steps of 2^e
     e = torch.where(m == 0, torch.full_like(e, -100), e)
     a = torch.ldexp(y.abs(), -e[..., None])
     step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
@@ -459,7 +459,7 @@ def _exact_store(s):
         m = y.abs().amax(-1, keepdim=True)
         e = torch.floor(torch.log2(m))
         e = torch.where(torch.exp2(e + 1) <= m, e + 1, torch.where(torch.exp2(e) > m, e - 1, e))
-        e = torch.where(m > 1.75 * torch.exp2(e), e - 1, e - 2).clamp(min=-100)
+        e = torch.where(m > 1.75 * torch.exp2(e), e - 1, e - 2).clamp(-100, 125)
         z = y.abs() / torch.exp2(e)
         # the nearest of the even codes' values, unless one of the odd codes' is nearer
         best, near = torch.zeros_like(z), z
