@@ -396,6 +396,101 @@ LOCOCO_API lococo_status lococo_sequence_backward(const lococo_config* cfg, cons
                                                   float* d_conv_w, float* d_conv_b, void* workspace,
                                                   size_t ws_bytes, void* stream);
 
+/* ---- Paged 4-bit rows: many requests of different lengths in one call -------------------------------------------------------
+ *
+ * A server keeps, for each request, rows of K and V that do not change any more: the compressed memory a scan left (cache->k,
+ * cache->v) and the rows of the tokens since, or a whole uncompressed context.  Here such rows are held in 4 bits, in pages of
+ * page_rows rows that a request owns through its row of a table, and the calls take requests of any lengths side by side:
+ *
+ *   lococo_pages_plan    from the requests' lengths: pages handed out and taken back, every new row's slot and position
+ *   lococo_pages_store   new rows (or a memory's slots) to 4 bits, to their slots; lococo_pages_load the way back
+ *   lococo_pages_attn    attention of the new rows' queries over all rows of their request
+ *
+ * Format.  32 consecutive values of a row share a scale byte e, which stands for 2^(e - 127); a value is a sign and one of the
+ * eight magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6 times that scale (codes 0 .. 7, + 8 for the sign).  Storing takes, for the largest
+ * magnitude a of the 32, 2^E with E = floor(log2 a) - 2, one more if a exceeds 7/4 of its power of two, -100 at least and 125 at most, and the
+ * code nearest to value / 2^E, ties to the even code.  32 values that hold an infinity or a NaN get the byte 255 and stand for
+ * NaN all of them.  Reading gives exactly scale times magnitude in either storage type (magnitudes of scale bytes below 2 apart,
+ * which storing never writes).
+ *   codes   [n_pages][n_kv_heads][page_rows][head_dim / 2] bytes, value 2i of a row in the low four bits of its byte i
+ *   scales  [n_pages][n_kv_heads][head_dim / 32][page_rows] bytes
+ * The slot of row r of page p is p * page_rows + r.  What slots that nobody holds contain is never read into a result.
+ *
+ * Device arrays of numbers (tables, slots, ...) are read when the kernels run, so the host checks their pointers only; numbers in
+ * them that make no sense are cut to their range or leave rows out, and never take an access outside the arrays described. */
+typedef struct lococo_pages {
+  uint32_t struct_size;   /* sizeof(lococo_pages)                                                            */
+  int32_t dtype;          /* LOCOCO_F32 / LOCOCO_BF16: storage type of q, k, v and o rows                    */
+  int32_t n_q_heads;      /* multiple of n_kv_heads; query head h reads kv head h / group                    */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* a multiple of 32, at most 256                                                   */
+  int32_t page_rows;      /* a power of two, 16 .. 1024                                                      */
+  int32_t n_pages;        /* n_pages * page_rows < 2^30                                                      */
+  float attn_scale;       /* 0 => 1/sqrt(head_dim)                                                           */
+  uint8_t* k_codes;       /* device, 16-byte aligned                                                         */
+  uint8_t* k_scales;
+  uint8_t* v_codes;
+  uint8_t* v_scales;
+} lococo_pages;
+
+/* The plan of a turn, on the GPU: n requests (at most 4096), request i holding held[i] rows and bringing new_rows[i] more, or
+ * new_rows[i] < 0: the request is at its end.  Requests are served in order:
+ *   - its rows are rows starts[i] .. starts[i + 1] - 1 of the call, which has room for `tokens` of them (0 .. 2^30 - 2);
+ *   - a request that needs more pages than it has takes the next ones of the ring, in order, and enters them in its row of
+ *     `tables` (table_pages entries); row x of it, at position held[i] + x, gets its slot and its position written;
+ *   - a request whose rows pass `tokens`, whose pages pass table_pages, or whose pages together with those all requests before
+ *     it asked for are more than the ring had at the start of the call, is refused as a whole: it takes no page, held_after is
+ *     held, the slots and positions of its rows are -1 (its place in the call stays);
+ *   - a request at its end gives its pages back behind the ring's last one, its held_after is 0.  Pages given back can be taken
+ *     from the next call on.
+ * Rows of the call behind the last request's get -1.  ring [n_pages] holds the free pages: the entries ends[0] .. ends[1] - 1,
+ * counted modulo n_pages; a fresh pool is 0, 1, .. n_pages - 1 with ends = {0, n_pages}.
+ *   in      new_rows, held [n]; ends [2]
+ *   in out  tables [n][table_pages], ring [n_pages]
+ *   out     held_after [n], ends_after [2], starts [n + 1], slots, positions [tokens], totals [4]: rows placed, pages taken,
+ *           pages given back, requests refused.  held_after, ends_after and starts are not held, ends or new_rows: a turn's
+ *           plan can be repeated.
+ * All numbers are the same from call to call (nothing depends on the order workgroups run in).  Of `pages` page_rows and n_pages
+ * are used; the arrays may be NULL. */
+LOCOCO_API lococo_status lococo_pages_plan(const lococo_pages* pages, int32_t n, int32_t tokens, int32_t table_pages,
+                                           const int32_t* new_rows, const int32_t* held, int32_t* tables, int32_t* ring,
+                                           const int64_t* ends, int32_t* held_after, int64_t* ends_after, int32_t* starts,
+                                           int32_t* slots, int32_t* positions, int32_t* totals, void* stream);
+
+/* Rows of k and v, [b, n_kv_heads, rows_per_batch, head_dim] views holding `tokens` rows (row i of the call is row
+ * i % rows_per_batch of batch entry i / rows_per_batch), to 4 bits at slots[i]; a slot outside the pages (-1) leaves its row out.
+ * Two rows of a call must not share a slot; a call of no rows does nothing.  lococo_pages_load is the way back: rows at slots outside the pages become zeros. */
+LOCOCO_API lococo_status lococo_pages_store(const lococo_pages* pages, const lococo_tensor* k, const lococo_tensor* v,
+                                            int32_t rows_per_batch, int32_t tokens, const int32_t* slots, void* stream);
+LOCOCO_API lococo_status lococo_pages_load(const lococo_pages* pages, const int32_t* slots, int32_t rows_per_batch,
+                                           int32_t tokens, const lococo_tensor* k, const lococo_tensor* v, void* stream);
+
+/* The requests of an attention call, as lococo_pages_plan leaves them. */
+typedef struct lococo_requests {
+  int32_t n;              /* requests, 1 .. 4096                                                             */
+  int32_t tokens;         /* rows of q and o                                                                 */
+  int32_t table_pages;    /* entries of a table; table_pages * page_rows < 2^30                              */
+  int32_t max_new;        /* no request has more new rows, of those it is the caller's promise: what is over
+                             is left unwritten                                                               */
+  int32_t max_held;       /* about the most rows a request holds: only how the work is dealt out goes by it  */
+  const int32_t* tables;  /* device [n][table_pages]                                                         */
+  const int32_t* starts;  /* device [n + 1], not decreasing: request i's queries are rows starts[i] ..       */
+  const int32_t* held;    /* device [n]: rows held, the new ones among them (the plan's held_after)          */
+} lococo_requests;
+
+/* o = Attn(Q, K, V) of every request over its own rows: query x of a request with `new` queries stands at position
+ * held - new + x and sees the rows up to and at its position (Eq. 1 with the cache in front, as in lococo_attn_only); a compressed
+ * memory stored ahead of the tokens is thus seen by all of them.  A query that sees nothing (held below new) gets zeros, rows of o
+ * that no request has are not written, rows whose table entry is no page are left out.  q and o: [b, n_q_heads, rows_per_batch,
+ * head_dim] views of requests->tokens rows counted as in lococo_pages_store; o must not alias q.  Softmax and sums in fp32,
+ * operands as stored: with LOCOCO_BF16 probabilities enter their product rounded to bf16, with LOCOCO_F32 nothing is rounded on
+ * the way.  A visible row's NaN reaches the results of the queries that see it and no others.
+ * workspace: device, 256-byte aligned, lococo_pages_workspace_bytes of the same sizes (may be 0). */
+LOCOCO_API lococo_status lococo_pages_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out);
+LOCOCO_API lococo_status lococo_pages_attn(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
+                                           const lococo_tensor* o, int32_t rows_per_batch, void* workspace, size_t ws_bytes,
+                                           void* stream);
+
 /* Optional per-kernel timing.  Between lococo_timing_begin() and
  * lococo_timing_end() every kernel the library launches (from any thread) is
  * bracketed by a pair of HIP events recorded on the stream it is launched on.

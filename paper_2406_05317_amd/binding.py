@@ -28,7 +28,9 @@ EXPORTS = ["lococo_plan", "lococo_workspace_bytes", "lococo_attn_only", "lococo_
            "lococo_prepare_filters", "lococo_backward_workspace_bytes", "lococo_segment_step_backward",
            "lococo_measure_peaks", "lococo_debug_option", "lococo_describe_path",
            "lococo_segment_step_noalloc", "lococo_sequence_backward_workspace_bytes",
-           "lococo_sequence_backward"]
+           "lococo_sequence_backward",
+           "lococo_pages_plan", "lococo_pages_store", "lococo_pages_load", "lococo_pages_workspace_bytes",
+           "lococo_pages_attn"]
 
 
 class lococo_config(C.Structure):
@@ -70,6 +72,17 @@ class lococo_path_info(C.Structure):
     _fields_ = [("path", C.c_int32), ("compute_units", C.c_int32), ("tile_slots", C.c_int32),
                 ("scan_groups", C.c_int32), ("scan_resident_limit", C.c_int32), ("position_split", C.c_int32),
                 ("step_pipeline", C.c_int32), ("reserved", C.c_int32)]
+
+
+class lococo_pages(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32), ("attn_scale", C.c_float),
+                ("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class lococo_requests(C.Structure):
+    _fields_ = [("n", C.c_int32), ("tokens", C.c_int32), ("table_pages", C.c_int32), ("max_new", C.c_int32),
+                ("max_held", C.c_int32), ("tables", C.c_void_p), ("starts", C.c_void_p), ("held", C.c_void_p)]
 
 
 class LococoError(RuntimeError):
@@ -114,6 +127,12 @@ def lib():
                                            C.POINTER(C.c_double)]
         L.lococo_debug_option.argtypes = [C.c_int32, C.c_int64]
         L.lococo_describe_path.argtypes = [cfgp, C.c_int32, C.POINTER(lococo_path_info)]
+        pgp, rqp, tp, i32 = C.POINTER(lococo_pages), C.POINTER(lococo_requests), C.POINTER(lococo_tensor), C.c_int32
+        L.lococo_pages_plan.argtypes = [pgp, i32, i32, i32] + [C.c_void_p] * 12
+        L.lococo_pages_store.argtypes = [pgp, tp, tp, i32, i32, C.c_void_p, C.c_void_p]
+        L.lococo_pages_load.argtypes = [pgp, C.c_void_p, i32, i32, tp, tp, C.c_void_p]
+        L.lococo_pages_workspace_bytes.argtypes = [pgp, rqp, C.POINTER(C.c_size_t)]
+        L.lococo_pages_attn.argtypes = [pgp, rqp, tp, tp, i32, C.c_void_p, C.c_size_t, C.c_void_p]
         L.lococo_timing_begin.argtypes = []
         L.lococo_timing_end.argtypes = [C.POINTER(lococo_kernel_time), C.POINTER(C.c_int32)]
         for n in EXPORTS[:6] + EXPORTS[8:]:
@@ -227,6 +246,26 @@ class Cache:
         self.c.len = length
 
 
+class Pages:
+    """Device arrays of paged 4-bit rows and their description (lococo_pages in lococo.h): `n_pages` pages of `page_rows` rows
+    of every kv head.  Nobody owns a page at first: see fresh_ring."""
+
+    def __init__(self, *, dtype: torch.dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, page_rows: int, n_pages: int,
+                 attn_scale: float = 0.0, device="cuda"):
+        codes, scales = (n_pages, n_kv_heads, page_rows, head_dim // 2), (n_pages, n_kv_heads, head_dim // 32, page_rows)
+        self.k_codes, self.v_codes = (torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2))
+        self.k_scales, self.v_scales = (torch.zeros(scales, dtype=torch.uint8, device=device) for _ in range(2))
+        self.c = lococo_pages(C.sizeof(lococo_pages), _dtype_code(dtype), n_q_heads, n_kv_heads, head_dim, page_rows, n_pages,
+                              attn_scale, self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
+                              self.v_scales.data_ptr())
+        self.dtype, self.device = dtype, device
+
+    def fresh_ring(self):
+        """(ring, ends) with every page free, as lococo_pages_plan takes them."""
+        return (torch.arange(self.c.n_pages, dtype=torch.int32, device=self.device),
+                torch.tensor([0, self.c.n_pages], dtype=torch.int64, device=self.device))
+
+
 def lococo_version() -> str:
     return lib().lococo_version().decode()
 
@@ -334,6 +373,62 @@ def lococo_sequence_backward(cfg, q, k, v, B: int, conv_w, conv_b, cache: Cache,
         _ptr(d_conv_b), _ptr(workspace), ws_bytes, _stream()))
 
 
+def _numbers(dtype, **arrays):
+    for name, t in arrays.items():
+        assert t.dtype == dtype and t.is_contiguous() and t.is_cuda, f"{name}: expected contiguous {dtype} on the device"
+
+
+def lococo_pages_plan(pages: Pages, new_rows, held, tables, ring, ends, held_after, ends_after, starts, slots, positions, totals):
+    """Pages, slots and positions of a turn from its requests' lengths (all arrays on the device: int32, ends int64)."""
+    _numbers(torch.int32, new_rows=new_rows, held=held, tables=tables, ring=ring, held_after=held_after, starts=starts, slots=slots,
+             positions=positions, totals=totals)
+    _numbers(torch.int64, ends=ends, ends_after=ends_after)
+    n, width = tables.shape
+    assert new_rows.numel() == held.numel() == held_after.numel() == n and starts.numel() == n + 1
+    assert ring.numel() == pages.c.n_pages and ends.numel() == ends_after.numel() == 2
+    assert slots.numel() == positions.numel() and totals.numel() == 4
+    _check(lib().lococo_pages_plan(C.byref(pages.c), n, slots.numel(), width, *(_ptr(t) for t in (
+        new_rows, held, tables, ring, ends, held_after, ends_after, starts, slots, positions, totals)), _stream()))
+
+
+def _rows(pages: Pages, t: torch.Tensor, heads: int) -> lococo_tensor:
+    assert t.dtype == pages.dtype and t.is_cuda and t.shape[1] == heads and t.shape[3] == pages.c.head_dim
+    return _tensor(t)
+
+
+def lococo_pages_store(pages: Pages, k, v, slots):
+    """k, v [b, n_kv_heads, t, d] to 4 bits, row (b, t) at slots[b * T + t]."""
+    _numbers(torch.int32, slots=slots)
+    assert k.shape == v.shape and slots.numel() == k.shape[0] * k.shape[2]
+    x, y = _rows(pages, k, pages.c.n_kv_heads), _rows(pages, v, pages.c.n_kv_heads)
+    _check(lib().lococo_pages_store(C.byref(pages.c), C.byref(x), C.byref(y), max(k.shape[2], 1), slots.numel(), _ptr(slots), _stream()))
+
+
+def lococo_pages_load(pages: Pages, slots, k, v):
+    """The rows at `slots` into k, v [b, n_kv_heads, t, d]."""
+    _numbers(torch.int32, slots=slots)
+    assert k.shape == v.shape and slots.numel() == k.shape[0] * k.shape[2]
+    x, y = _rows(pages, k, pages.c.n_kv_heads), _rows(pages, v, pages.c.n_kv_heads)
+    _check(lib().lococo_pages_load(C.byref(pages.c), _ptr(slots), max(k.shape[2], 1), slots.numel(), C.byref(x), C.byref(y), _stream()))
+
+
+def lococo_pages_workspace_bytes(pages: Pages, n: int, tokens: int, max_new: int, max_held: int, table_pages: int = 1) -> int:
+    r, out = lococo_requests(n, tokens, table_pages, max_new, max_held, None, None, None), C.c_size_t(0)
+    _check(lib().lococo_pages_workspace_bytes(C.byref(pages.c), C.byref(r), C.byref(out)))
+    return out.value
+
+
+def lococo_pages_attn(pages: Pages, q, o, tables, starts, held, max_new: int, max_held: int, workspace=None):
+    """Attention of the requests' new rows q [b, n_q_heads, t, d] over all rows of their request, into o."""
+    _numbers(torch.int32, tables=tables, starts=starts, held=held)
+    n, width = tables.shape
+    assert q.shape == o.shape and starts.numel() == n + 1 and held.numel() == n
+    x, y = _rows(pages, q, pages.c.n_q_heads), _rows(pages, o, pages.c.n_q_heads)
+    r = lococo_requests(n, q.shape[0] * q.shape[2], width, max_new, max_held, _ptr(tables), _ptr(starts), _ptr(held))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().lococo_pages_attn(C.byref(pages.c), C.byref(r), C.byref(x), C.byref(y), max(q.shape[2], 1), _ptr(workspace), ws_bytes, _stream()))
+
+
 def lococo_scan_status(cfg, workspace) -> int:
     """Synchronises; 0 = fine, 1 = a chain wait inside the one-launch scan of the lococo_sequence_forward or
     lococo_sequence_backward call that had this workspace gave up: its results are invalid."""
@@ -380,6 +475,12 @@ def workspace(cfg, L: int, B: int, history: bool = False, device="cuda") -> torc
     """Allocate (through torch) the workspace a call with these sizes needs."""
     n = lococo_workspace_bytes(cfg, L, B, history)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device) if n else None
+
+
+def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int) -> torch.Tensor | None:
+    """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes or smaller batches of them."""
+    need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
+    return torch.empty(need, dtype=torch.uint8, device=pages.device) if need else None
 
 
 def config_for(w, impl: int = 0, **over) -> lococo_config:

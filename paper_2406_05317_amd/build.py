@@ -17,7 +17,7 @@ LIB = os.path.join(PKG, "liblococo.so")
 
 SOURCES = ["api.cpp", "generic_kernels.hip", "scan_small.hip", "compress_mfma.hip", "compress_step.hip", "attn_mfma.hip", "attn_decode.hip",
            "bwd_attn_mfma.hip", "bwd_conv_mfma.hip",
-           "backward_generic.hip", "tiled_mfma.hip", "peaks.hip"]
+           "backward_generic.hip", "tiled_mfma.hip", "pages.hip", "pages_attn.hip", "peaks.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -37,7 +37,8 @@ EXTRA = {"compress_mfma.hip": COMPRESS, "compress_step.hip": COMPRESS,
          # accumulators in ordinary registers: the softmax reads the scores where the MFMA left them
          "attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "bwd_attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "bwd_conv_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "bwd_conv_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "pages_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:

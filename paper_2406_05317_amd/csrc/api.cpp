@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "lococo_internal.h"
+#include "pages.h"
 
 using namespace lococo;
 
@@ -62,11 +63,12 @@ lococo_status hip_fail(hipError_t e, const char* what) {
 // ---- optional per-kernel timing with HIP events (lococo_timing_begin / _end)
 enum KernelId { K_ATTN_GENERIC, K_FILL, K_CONV_GENERIC, K_NORM_GENERIC, K_MIX_GENERIC,
                 K_REPACK, K_COMPRESS_MFMA, K_ATTN_MFMA, K_ATTN_DECODE, K_ATTN_COLSUM, K_CONV_MFMA, K_MIX_MFMA,
-                K_COMPRESS_SMALL, K_BWD_WALK, K_COUNT };
+                K_COMPRESS_SMALL, K_BWD_WALK, K_PAGES_PLAN, K_PAGES_STORE, K_PAGES_LOAD, K_PAGES_ATTN, K_COUNT };
 const char* const kKernelNames[K_COUNT] = {"attn_generic", "fill", "conv_logits_generic",
                                            "normalise_generic", "mix_generic", "repack_filters",
                                            "compress_mfma", "attn_mfma", "attn_decode", "attn_colsum",
-                                           "conv_logits_mfma", "mix_mfma", "compress_small", "bwd_walk"};
+                                           "conv_logits_mfma", "mix_mfma", "compress_small", "bwd_walk",
+                                           "pages_plan", "pages_store", "pages_load", "pages_attn"};
 struct TimedLaunch { int id; hipEvent_t start, stop; };
 std::mutex g_timing_mu;
 bool g_timing_on = false;
@@ -1734,6 +1736,188 @@ lococo_status lococo_sequence_backward(const lococo_config* cfg, const lococo_qk
     }
     w1 = w0;
   }
+  return LOCOCO_OK;
+}
+
+}  // extern "C"
+
+// ---- paged 4-bit rows
+namespace {
+
+lococo_status check_pages(const lococo_pages* p, bool arrays) {
+  if (!p) return fail(LOCOCO_EINVAL, "pages is NULL");
+  if (p->struct_size != sizeof(lococo_pages))
+    return fail(LOCOCO_EINVAL, "pages.struct_size is %u, this library expects %zu", p->struct_size, sizeof(lococo_pages));
+  if (p->page_rows <= 0 || p->n_pages <= 0) return fail(LOCOCO_EINVAL, "page_rows and n_pages must be positive");
+  if (p->page_rows < kPagesMinRows || p->page_rows > kPagesMaxRows || (p->page_rows & (p->page_rows - 1)))
+    return fail(LOCOCO_EUNSUPPORTED, "page_rows %d is not a power of two from %d to %d", p->page_rows, kPagesMinRows, kPagesMaxRows);
+  if ((int64_t)p->n_pages * p->page_rows >= kPagesCap)
+    return fail(LOCOCO_EUNSUPPORTED, "n_pages * page_rows must be below 2^30 - 1");
+  if (!arrays) return LOCOCO_OK;
+  if (p->dtype != LOCOCO_F32 && p->dtype != LOCOCO_BF16)
+    return fail(LOCOCO_EINVAL, "pages.dtype %d is neither LOCOCO_F32 nor LOCOCO_BF16", p->dtype);
+  if (p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0) return fail(LOCOCO_EINVAL, "head counts and head_dim must be positive");
+  if (p->n_q_heads % p->n_kv_heads)
+    return fail(LOCOCO_EINVAL, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads);
+  if (p->n_q_heads > 65535) return fail(LOCOCO_EUNSUPPORTED, "n_q_heads above 65535");
+  if (p->head_dim % 32 || p->head_dim > kPagesMaxHeadDim)
+    return fail(LOCOCO_EUNSUPPORTED, "head_dim %d is not a multiple of 32 up to %d", p->head_dim, kPagesMaxHeadDim);
+  if (!(p->attn_scale >= 0.f) || std::isinf(p->attn_scale)) return fail(LOCOCO_EINVAL, "attn_scale must be finite and >= 0");
+  const uint8_t* a[4] = {p->k_codes, p->k_scales, p->v_codes, p->v_scales};
+  for (int i = 0; i < 4; ++i) {
+    if (!a[i]) return fail(LOCOCO_EINVAL, "a pointer to the pages is NULL");
+    if ((uintptr_t)a[i] & 15) return fail(LOCOCO_EINVAL, "the arrays of the pages must be 16-byte aligned");
+    for (int j = 0; j < i; ++j)
+      if (a[i] == a[j]) return fail(LOCOCO_EINVAL, "the arrays of the pages alias each other");
+  }
+  return LOCOCO_OK;
+}
+
+PagesView pages_view(const lococo_pages* p) {
+  int shift = 0;
+  while ((1 << shift) < p->page_rows) ++shift;
+  const float scale = p->attn_scale > 0.f ? p->attn_scale : 1.f / std::sqrt((float)p->head_dim);
+  return PagesView{p->k_codes, p->k_scales, p->v_codes, p->v_scales, p->n_pages, p->page_rows, shift, p->n_q_heads, p->n_kv_heads,
+                   p->n_q_heads / p->n_kv_heads, p->head_dim, scale};
+}
+
+lococo_status check_rows(const lococo_pages* p, const lococo_tensor* t, const char* name, int32_t rows_per_batch, int32_t tokens) {
+  if (!t) return fail(LOCOCO_EINVAL, "%s is NULL", name);
+  if (rows_per_batch <= 0 || tokens < 0) return fail(LOCOCO_EINVAL, "rows_per_batch must be positive and tokens not negative");
+  if (tokens >= kPagesCap) return fail(LOCOCO_EUNSUPPORTED, "tokens must be below 2^30 - 1");
+  if (tokens == 0) return LOCOCO_OK;                 // an empty tensor has no address
+  lococo_config c{};
+  c.dtype = p->dtype;
+  c.head_dim = p->head_dim;
+  return check_tensor(&c, *t, name, tokens);
+}
+
+RowsView rows_view(const lococo_tensor* t, int32_t rows_per_batch) {
+  return RowsView{t->p, t->stride_b, t->stride_h, t->stride_t, rows_per_batch};
+}
+
+lococo_status check_requests(const lococo_pages* p, const lococo_requests* r, bool arrays) {
+  if (!r) return fail(LOCOCO_EINVAL, "requests is NULL");
+  if (r->n <= 0 || r->tokens < 0 || r->table_pages <= 0 || r->max_new < 0 || r->max_held < 0)
+    return fail(LOCOCO_EINVAL, "n and table_pages must be positive, tokens, max_new and max_held not negative");
+  if (r->n > kPagesMaxRequests) return fail(LOCOCO_EUNSUPPORTED, "more than %d requests", kPagesMaxRequests);
+  if (r->tokens >= kPagesCap || (int64_t)r->table_pages * p->page_rows >= kPagesCap)
+    return fail(LOCOCO_EUNSUPPORTED, "tokens and table_pages * page_rows must be below 2^30 - 1");
+  if ((int64_t)r->max_new * r->n < r->tokens) return fail(LOCOCO_EINVAL, "max_new * n is below tokens");
+  if (arrays) {
+    if (!r->tables || !r->starts || !r->held) return fail(LOCOCO_EINVAL, "an array of the requests is NULL");
+    if (((uintptr_t)r->tables | (uintptr_t)r->starts | (uintptr_t)r->held) & 3)
+      return fail(LOCOCO_EINVAL, "arrays of the requests must be 4-byte aligned");
+  }
+  return LOCOCO_OK;
+}
+
+PagesAttnArgs pages_attn_args(const lococo_pages* p, const lococo_requests* r) {
+  PagesAttnArgs a{};
+  a.pg = pages_view(p);
+  a.n = r->n;
+  a.tokens = r->tokens;
+  a.table_pages = r->table_pages;
+  a.max_new = r->max_new;
+  a.max_held = r->max_held;
+  a.tables = r->tables;
+  a.starts = r->starts;
+  a.held = r->held;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+lococo_status lococo_pages_plan(const lococo_pages* pages, int32_t n, int32_t tokens, int32_t table_pages, const int32_t* new_rows,
+                                const int32_t* held, int32_t* tables, int32_t* ring, const int64_t* ends, int32_t* held_after,
+                                int64_t* ends_after, int32_t* starts, int32_t* slots, int32_t* positions, int32_t* totals,
+                                void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, false))) return st;
+  if (n <= 0 || tokens < 0 || table_pages <= 0) return fail(LOCOCO_EINVAL, "n and table_pages must be positive, tokens not negative");
+  if (n > kPagesMaxRequests) return fail(LOCOCO_EUNSUPPORTED, "more than %d requests", kPagesMaxRequests);
+  if (tokens >= kPagesCap || (int64_t)table_pages * pages->page_rows >= kPagesCap)
+    return fail(LOCOCO_EUNSUPPORTED, "tokens and table_pages * page_rows must be below 2^30 - 1");
+  const void* in[] = {new_rows, held, tables, ring, ends, held_after, ends_after, starts, totals};
+  for (const void* p : in)
+    if (!p) return fail(LOCOCO_EINVAL, "an array of the plan is NULL");
+  if (tokens && (!slots || !positions)) return fail(LOCOCO_EINVAL, "slots and positions are NULL");
+  uintptr_t low = (uintptr_t)slots | (uintptr_t)positions;
+  for (const void* p : in) low |= (uintptr_t)p;
+  if ((low & 3) || (((uintptr_t)ends | (uintptr_t)ends_after) & 7))
+    return fail(LOCOCO_EINVAL, "arrays of the plan must be 4-byte aligned, ends and ends_after 8-byte");
+  // every workgroup reads these lists while the first one writes its results
+  const void* outs[] = {held_after, ends_after, starts, totals, slots, positions};
+  for (const void* o : outs)
+    for (const void* i : {(const void*)new_rows, (const void*)held, (const void*)tables, (const void*)ring, (const void*)ends})
+      if (o && o == i) return fail(LOCOCO_EINVAL, "an output of the plan aliases an input");
+  PagesView v = pages_view(pages);
+  PagesPlanArgs a{n, tokens, table_pages, v.page_rows, v.page_shift, v.n_pages, new_rows, held, tables, ring, ends, held_after,
+                  ends_after, starts, slots, positions, totals};
+  KTimer kt(K_PAGES_PLAN, (hipStream_t)stream);
+  HIP_TRY(launch_pages_plan(a, (hipStream_t)stream), "page plan launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_store(const lococo_pages* pages, const lococo_tensor* k, const lococo_tensor* v, int32_t rows_per_batch,
+                                 int32_t tokens, const int32_t* slots, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_rows(pages, k, "k", rows_per_batch, tokens)) ||
+      (st = check_rows(pages, v, "v", rows_per_batch, tokens)))
+    return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if (!slots || ((uintptr_t)slots & 3)) return fail(LOCOCO_EINVAL, "slots is NULL or not 4-byte aligned");
+  KTimer kt(K_PAGES_STORE, (hipStream_t)stream);
+  HIP_TRY(launch_pages_store(pages->dtype, pages_view(pages), rows_view(k, rows_per_batch), rows_view(v, rows_per_batch), tokens, slots,
+                             (hipStream_t)stream),
+          "store to pages launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_load(const lococo_pages* pages, const int32_t* slots, int32_t rows_per_batch, int32_t tokens,
+                                const lococo_tensor* k, const lococo_tensor* v, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_rows(pages, k, "k", rows_per_batch, tokens)) ||
+      (st = check_rows(pages, v, "v", rows_per_batch, tokens)))
+    return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if (!slots || ((uintptr_t)slots & 3)) return fail(LOCOCO_EINVAL, "slots is NULL or not 4-byte aligned");
+  if (k->p == v->p) return fail(LOCOCO_EINVAL, "k aliases v");
+  KTimer kt(K_PAGES_LOAD, (hipStream_t)stream);
+  HIP_TRY(launch_pages_load(pages->dtype, pages_view(pages), rows_view(k, rows_per_batch), rows_view(v, rows_per_batch), tokens, slots,
+                            (hipStream_t)stream),
+          "load from pages launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out) {
+  lococo_status st;
+  if (!out) return fail(LOCOCO_EINVAL, "out is NULL");
+  if ((st = check_pages(pages, true)) || (st = check_requests(pages, requests, false))) return st;
+  *out = align_up(pages_attn_workspace_bytes(pages->dtype, pages_attn_args(pages, requests)), 256);
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_attn(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
+                                const lococo_tensor* o, int32_t rows_per_batch, void* workspace, size_t ws_bytes, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_requests(pages, requests, true)) ||
+      (st = check_rows(pages, q, "q", rows_per_batch, requests->tokens)) ||
+      (st = check_rows(pages, o, "o", rows_per_batch, requests->tokens)))
+    return st;
+  if (requests->tokens == 0) return LOCOCO_OK;
+  if (o->p == q->p) return fail(LOCOCO_EINVAL, "o aliases q");
+  PagesAttnArgs a = pages_attn_args(pages, requests);
+  a.q = rows_view(q, rows_per_batch);
+  a.o = rows_view(o, rows_per_batch);
+  const size_t need = align_up(pages_attn_workspace_bytes(pages->dtype, a), 256);
+  if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
+    return fail(LOCOCO_EWORKSPACE, "attention over pages needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,
+                workspace ? ws_bytes : (size_t)0);
+  KTimer kt(K_PAGES_ATTN, (hipStream_t)stream);
+  HIP_TRY(launch_pages_attn(pages->dtype, a, workspace, (hipStream_t)stream), "attention over pages launch");
   return LOCOCO_OK;
 }
 

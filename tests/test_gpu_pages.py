@@ -1,0 +1,413 @@
+"""Paged 4-bit rows on the GPU against plain implementations in 64 bits: the page plan (whole numbers, equal), rows to 4 bits and back
+(equal), attention over the pages.
+
+Tolerances of the attention, per element, from the arithmetic the header promises: with A = sum p |v|,
+  bf16: probabilities and the result are rounded to 8 bits: 2^-9 A each; the fp32 part below them
+  both: a score's error is at most (d + 8) 2^-23 sum |q k| scale (products exact or rounded once, d additions, the factor), and as much
+        again for the argument of the exponential; p takes it twice (itself and the sum); the sums of up to n terms: (n + 64) 2^-23 A."""
+import math
+import random
+
+import pytest
+import torch
+
+import pages_util as pu
+from paper_2406_05317_amd import binding as lb
+
+pytestmark = pytest.mark.gpu
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+# ---- the plan
+def run_plan(n_pages, R, tokens, new, held, tables, ring, ends):
+    pages = lb.Pages(dtype=torch.bfloat16, n_q_heads=1, n_kv_heads=1, head_dim=32, page_rows=R, n_pages=n_pages)
+    t = {k: torch.tensor(v, **I32) for k, v in dict(new=new, held=held, tables=tables, ring=ring).items()}
+    e, n = torch.tensor(ends, dtype=torch.int64, device="cuda"), len(new)
+    ea = torch.zeros(2, dtype=torch.int64, device="cuda")
+    out = {k: torch.full((m,), -77, **I32) for k, m in dict(held=n, starts=n + 1, slots=tokens, positions=tokens, totals=4).items()}
+    lb.lococo_pages_plan(pages, t["new"], t["held"], t["tables"], t["ring"], e, out["held"], ea, out["starts"], out["slots"],
+                         out["positions"], out["totals"])
+    got = {k: v.tolist() for k, v in out.items()}
+    return dict(got, ends=ea.tolist(), tables=t["tables"].tolist(), ring=t["ring"].tolist())
+
+
+def draw_plan(seed, n, R, spare, ends_share, pad=5):
+    r = random.Random(seed)
+    held = [r.choice([0, 1, R - 1, R, R + 1, r.randint(0, 9 * R)]) for _ in range(n)]
+    new = [-1 if r.random() < ends_share else r.choice([0, 1, 1, 1, R, r.randint(0, 3 * R)]) for _ in range(n)]
+    used = sum(-(-h // R) for h in held)
+    need = sum(-(-(h + w) // R) - -(-h // R) for h, w in zip(held, new) if w > 0)
+    free = int(need * spare) + (2 if spare >= 1 else 0)
+    P = used + free + 1
+    ids = list(range(P - 1))
+    r.shuffle(ids)
+    width = max(-(-(h + max(w, 0)) // R) for h, w in zip(held, new)) + r.randint(0, 1)
+    tables = []
+    for h in held:
+        k = -(-h // R)
+        tables.append(ids[:k] + [-5] * (max(width, 10) - k))
+        ids = ids[k:]
+    head = r.randint(0, 4 * P)
+    ring = [-9] * P
+    for j, p in enumerate(ids[:free]):
+        ring[(head + j) % P] = p
+    return P, R, sum(max(w, 0) for w in new) + pad, new, held, tables, ring, [head, head + len(ids[:free])]
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 255, 257, 1000, 4096])
+@pytest.mark.parametrize("spare,ends_share", [(1.0, 0.0), (1.0, 0.3), (0.5, 0.1), (0.0, 0.5)])
+def test_plan(n, spare, ends_share):
+    case = draw_plan(n, n, 16 if n % 2 else 64, spare, ends_share)
+    assert run_plan(*case) == pu.plan(*case)
+
+
+def test_plan_without_rows_and_with_too_little_room():
+    P, R, tokens, new, held, tables, ring, ends = draw_plan(5, 40, 16, 1.0, 0.3, pad=0)
+    only = [-1 if w < 0 else 0 for w in new]
+    assert run_plan(P, R, 0, only, held, tables, ring, ends) == pu.plan(P, R, 0, only, held, tables, ring, ends)
+    for room in (tokens // 2, 1, 0):                      # requests whose rows pass the room are refused
+        case = (P, R, room, new, held, tables, ring, ends)
+        assert run_plan(*case) == pu.plan(*case)
+    short = [t[:7] for t in tables]                       # requests whose pages pass the tables
+    held = [min(h, 7 * R) for h in held]
+    case = (P, R, tokens, new, held, short, ring, ends)
+    assert run_plan(*case) == pu.plan(*case)
+
+
+def test_plan_of_lengths_that_make_no_sense():
+    """Sums of huge lengths saturate and refuse; a negative or too large number of rows held is cut to its range."""
+    big = 2 ** 31 - 1
+    new, held = [3, big, big, 5, big - 7, 2], [10, 0, big, -4, 100, 20]
+    tables = [[i] * 8 for i in range(6)]
+    case = (50, 16, 64, new, held, tables, list(range(50)), [6, 50])
+    got, want = run_plan(*case), pu.plan(*case)
+    assert got["slots"][:3] == want["slots"][:3] and got["held"] == want["held"] and got["totals"] == want["totals"]
+    assert got["slots"] == want["slots"] and got["starts"] == want["starts"]
+    bad = (50, 16, 64, [20, 1], [10, 16], [[99] * 8, [-3] * 8], [77] * 50, [0, 50])      # entries that are no pages give no slots
+    got = run_plan(*bad)
+    assert got["slots"] == [-1] * 64 and got["positions"][:21] == list(range(10, 30)) + [16]
+
+
+def test_plan_turn_after_turn():
+    """Requests come, grow and end over many turns of one pool: no page belongs to two at once, none is lost."""
+    r, R, P, n, width = random.Random(3), 16, 60, 12, 8
+    held, tables, ring, ends = [0] * n, [[-1] * width for _ in range(n)], list(range(P)), [0, P]
+    for turn in range(40):
+        new = [-1 if h and r.random() < 0.2 else (r.randint(1, 40) if h == 0 else 1) if r.random() < 0.8 else 0 for h in held]
+        case = (P, R, sum(max(w, 0) for w in new) + 3, new, held, tables, ring, ends)
+        got = run_plan(*case)
+        assert got == pu.plan(*case), turn
+        held, tables, ring, ends = got["held"], got["tables"], got["ring"], got["ends"]
+        own = [p for h, t in zip(held, tables) for p in t[:-(-h // R)]]
+        free = [ring[j % P] for j in range(*ends)]
+        assert sorted(own + free) == list(range(P)), turn
+
+
+# ---- rows to 4 bits and back
+def make_rows(seed, shape, dtype):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * torch.exp2(torch.randint(-12, 12, shape[:-1] + (1,), generator=g).float())
+    flat = x.reshape(-1, 32)
+    if flat.shape[0] >= 8:
+        flat[0] = 0.0
+        flat[1] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0] * 2 + [-0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, -7.0] * 2)
+        flat[2] = flat[1] * 2.0 ** -99                    # scales at and below the smallest
+        flat[3] = flat[1] * 2.0 ** -104
+        flat[4] = torch.linspace(-1, 1, 32) * 3.0e38
+        flat[5] = torch.linspace(-7.5, 7.5, 32)           # top above 7/4 of its power of two
+        flat[6] = 1e-42 * torch.arange(32)                # subnormal numbers
+        flat[7, 5] = -0.0
+    return x.to(dtype)
+
+
+def arrays_of(pages):
+    return [t.cpu() for t in (pages.k_codes, pages.k_scales, pages.v_codes, pages.v_scales)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("b,t,heads,R", [(1, 1, 1, 16), (3, 37, 2, 16), (2, 130, 5, 64), (1, 70, 1, 1024)])
+def test_store_and_load(dtype, d, b, t, heads, R):
+    n_pages = b * t // R + 3
+    pages = lb.Pages(dtype=dtype, n_q_heads=heads, n_kv_heads=heads, head_dim=d, page_rows=R, n_pages=n_pages)
+    k, v = make_rows(1, (b, heads, t, d), dtype), make_rows(2, (b, heads, t, d), dtype)
+    perm = torch.randperm(n_pages * R, generator=torch.Generator().manual_seed(3))[:b * t].int()
+    before = arrays_of(pages)
+    lb.lococo_pages_store(pages, k.cuda(), v.cuda(), perm.cuda())
+    for x, codes, scales, c0, s0 in ((k, *arrays_of(pages)[:2], *before[:2]), (v, *arrays_of(pages)[2:], *before[2:])):
+        code, scale = pu.four_bits(x.transpose(1, 2).reshape(b * t, heads, d))
+        p, r = perm.long() // R, perm.long() % R
+        c0[p, :, r] = code[..., 0::2] | (code[..., 1::2] << 4)
+        s0[p, :, :, r] = scale
+        assert torch.equal(codes, c0) and torch.equal(scales, s0)       # and nothing else was written
+    ko, vo = torch.full_like(k, 7).cuda(), torch.full_like(v, 7).cuda()
+    lb.lococo_pages_load(pages, perm.cuda(), ko, vo)
+    for x, y in ((k, ko), (v, vo)):
+        assert torch.equal(y.cpu().double(), pu.values(*pu.four_bits(x)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_store_leaves_out_and_marks(dtype):
+    """Slots outside the pages; blocks with infinities or NaN; token-major rows and gaps between rows."""
+    heads, d, R, P, t = 3, 64, 16, 4, 20
+    pages = lb.Pages(dtype=dtype, n_q_heads=heads, n_kv_heads=heads, head_dim=d, page_rows=R, n_pages=P)
+    wide = make_rows(4, (1, t, heads + 1, d + 8), dtype).cuda()
+    k, v = wide[:, :, :heads, :d].transpose(1, 2), wide[:, :, 1:, 8:].transpose(1, 2)
+    k[0, 0, 0, 3], k[0, 1, 2, 40], v[0, 2, 3, 63] = math.inf, math.nan, -math.inf
+    slots = torch.arange(t, **I32)
+    slots[5], slots[6], slots[7] = -1, P * R, 2 ** 31 - 1
+    lb.lococo_pages_store(pages, k, v, slots)
+    outs = [torch.full((1, t, heads, d), 9.0, dtype=dtype, device="cuda").transpose(1, 2) for _ in range(2)]
+    lb.lococo_pages_load(pages, slots, *outs)
+    for x, y in zip((k.cpu(), v.cpu()), outs):
+        want = pu.values(*pu.four_bits(x))
+        want[:, :, 5:8] = 0.0
+        torch.testing.assert_close(y.cpu().double(), want, rtol=0, atol=0, equal_nan=True)
+    assert not pages.k_codes[0, :, 5:8].any() and not pages.k_scales[0, :, :, 5:8].any()
+
+
+def test_store_of_nothing():
+    pages = lb.Pages(dtype=torch.bfloat16, n_q_heads=2, n_kv_heads=2, head_dim=64, page_rows=16, n_pages=2)
+    none = torch.empty(1, 2, 0, 64, dtype=torch.bfloat16, device="cuda")
+    lb.lococo_pages_store(pages, none, none, torch.empty(0, **I32))
+    lb.lococo_pages_load(pages, torch.empty(0, **I32), none, none.clone())
+    assert not pages.k_codes.any()
+
+
+# ---- attention
+def make_batch(seed, dtype, kv, group, d, R, lens, gain=1.0, shape=None):
+    """(pages, q, tables, starts, held) of requests with (held, new) rows; what nobody holds is marked as NaN."""
+    g = torch.Generator().manual_seed(seed)
+    counts = [-(-h // R) for h, _ in lens]
+    P, width = sum(counts) + 2, max(counts + [1]) + 1
+    pages = lb.Pages(dtype=dtype, n_q_heads=kv * group, n_kv_heads=kv, head_dim=d, page_rows=R, n_pages=P)
+    ids = torch.randperm(P, generator=g).int()
+    tables, at = torch.full((len(lens), width), -1, dtype=torch.int32), 0
+    stale = torch.ones(P, R, dtype=torch.bool)
+    for i, ((h, _), c) in enumerate(zip(lens, counts)):
+        tables[i, :c] = ids[at:at + c]
+        stale[tables[i, :c].long()] = (torch.arange(c * R) >= h).reshape(c, R)
+        at += c
+    for codes, scales in ((pages.k_codes, pages.k_scales), (pages.v_codes, pages.v_scales)):
+        code, scale = pu.four_bits(torch.randn(P, kv, R, d, generator=g) * gain)
+        scale = scale.transpose(-1, -2).contiguous()
+        scale.masked_fill_(stale[:, None, None], 255)
+        codes.copy_(code[..., 0::2] | (code[..., 1::2] << 4))
+        scales.copy_(scale)
+    news = [w for _, w in lens]
+    starts = torch.tensor([sum(news[:i]) for i in range(len(lens) + 1)], dtype=torch.int32)
+    q = torch.randn(shape or (1, kv * group, sum(news), d), generator=g).to(dtype)
+    return pages, q, tables, starts, torch.tensor([h for h, _ in lens], dtype=torch.int32)
+
+
+def run_attn(pages, q, tables, starts, held, o=None, fill=5.0):
+    news = (starts[1:] - starts[:-1]).tolist()
+    o = torch.full_like(q, fill, device="cuda") if o is None else o
+    most = int(held.clamp(min=0).max())
+    ws = lb.pages_workspace(pages, len(held), q.shape[0] * q.shape[2], max(news), most)
+    if ws is not None:
+        ws.fill_(255)                                                  # what a workspace holds before a call may be anything
+    lb.lococo_pages_attn(pages, q.cuda() if not q.is_cuda else q, o, tables.cuda(), starts.cuda(), held.cuda(), max(news), most, ws)
+    return o
+
+
+def check_attn(pages, q, tables, starts, held, got, scale=None):
+    b, H, t, d = q.shape
+    c = pages.c
+    flat = q.cpu().transpose(0, 1).reshape(H, b * t, d)
+    o, mass, size = pu.attention(flat, tables, starts.tolist(), held.tolist(), arrays_of(pages), c.page_rows, H // c.n_kv_heads,
+                                 scale or 1.0 / math.sqrt(d))
+    got = got.cpu().double().transpose(0, 1).reshape(H, b * t, d)
+    n = max(1, int(held.max()))
+    rel = 4 * (d + 8) * 2.0 ** -23 * size[..., None] + (n + 64) * 2.0 ** -23
+    if q.dtype == torch.bfloat16:
+        rel = rel + 2.0 ** -8
+    real = starts.tolist()[-1]
+    o, got, tol = o[:, :real], got[:, :real], (rel * mass)[:, :real] + 1e-30
+    assert torch.equal(torch.isnan(o), torch.isnan(got))
+    bad = (got - o).abs() > tol
+    bad &= ~torch.isnan(o)
+    assert not bad.any(), (bad.nonzero()[:5].tolist(), ((got - o).abs() / tol)[bad].max().item())
+
+
+SHAPES = [  # kv, group, d, R
+    (2, 1, 128, 64), (1, 4, 128, 16), (2, 3, 64, 32), (1, 8, 64, 128), (1, 16, 128, 64), (1, 32, 64, 16), (2, 2, 96, 16), (1, 5, 256, 64),
+    (1, 1, 32, 1024)]
+LENGTHS = [
+    [(1, 1)], [(2, 1), (63, 1), (64, 1), (65, 1), (200, 1)], [(1, 1), (16, 16), (17, 3), (300, 2)],
+    [(0, 1), (3, 5), (40, 0), (100, 1), (0, 0), (129, 2)],             # nothing held, fewer rows than queries, no queries
+    [(150, 70), (33, 33), (500, 1)], [(700, 130)]]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,group,d,R", SHAPES)
+@pytest.mark.parametrize("lens", range(len(LENGTHS)))
+def test_attention(dtype, kv, group, d, R, lens):
+    batch = make_batch(lens, dtype, kv, group, d, R, LENGTHS[lens])
+    print(dtype, kv, group, d, R, LENGTHS[lens], flush=True)
+    check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,group,d,R,lens", [
+    (2, 4, 128, 64, [(5000, 1), (1, 1), (1023, 1)]), (1, 1, 128, 16, [(9001, 1)]), (1, 2, 64, 32, [(4097, 7), (2500, 2)]),
+    (1, 4, 128, 64, [(3000, 40), (10, 3)]), (2, 1, 64, 128, [(2100, 90)])])
+def test_attention_over_long_contexts(dtype, kv, group, d, R, lens):
+    """Lengths where the rows of one request are shared out between workgroups and their results joined."""
+    batch = make_batch(11, dtype, kv, group, d, R, lens)
+    check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+def test_attention_with_peaked_rows(dtype, d):
+    """Scores of several hundred: the running maximum moves, and by much."""
+    batch = make_batch(21, dtype, 1, 2, d, 16, [(300, 1), (600, 40), (97, 5)], gain=40.0)
+    check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+@pytest.mark.parametrize("new", [1, 4, 50])
+def test_attention_keeps_nan_where_it_is_seen(dtype, d, new):
+    """A marked block of K reaches every query that sees its row, one of V those queries' 32 columns; later rows' marks no earlier query."""
+    pages, q, tables, starts, held = make_batch(31, dtype, 2, 2, d, 16, [(200, new), (90, new), (120, new)])
+    page = lambda i, r: (int(tables[i, r // 16]), r % 16)
+    p, r = page(0, 199)
+    pages.v_scales[p, 1, 1, r] = 255                                   # the last row of request 0: its last query only
+    p, r = page(1, 40)
+    pages.v_scales[p, 0, 0, r] = 255                                   # seen by all of request 1's
+    if new > 1:
+        p, r = page(2, 118)
+        pages.k_scales[p, 0, 1, r] = 255                               # the last two queries of request 2
+    batch = (pages, q, tables, starts, held)
+    got = run_attn(*batch)
+    assert torch.isnan(got).any() and not torch.isnan(got).all()
+    check_attn(*batch, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_leaves_out_what_is_no_page(dtype, new):
+    pages, q, tables, starts, held = make_batch(41, dtype, 1, 2, 128, 16, [(200, new), (64, new), (300, new)])
+    tables[0, 3], tables[1, :], tables[2, 0], tables[2, 18] = -1, 10 ** 6, 2 ** 31 - 1, -(2 ** 31)
+    held[2] = 2 ** 31 - 1 if new == 1 else 300
+    if new == 1:
+        tables[2, 19:] = -1
+        held[2] = tables.shape[1] * 16                                 # as much as a table can hold
+    batch = (pages, q, tables, starts, held)
+    check_attn(*batch, run_attn(*batch))
+    held2 = held.clone()
+    held2[2] = 2 ** 31 - 1                                             # more is cut to that
+    if new == 1:
+        assert torch.equal(run_attn(pages, q, tables, starts, held2), run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+def test_attention_views_scale_and_rows_of_nobody(dtype, d):
+    """[n, heads, 1, d] and token-major views, a scale of the caller's, rows of o behind the last request, another stream."""
+    lens = [(50, 1), (7, 1), (130, 1), (64, 1)]
+    pages, q, tables, starts, held = make_batch(51, dtype, 2, 2, d, 16, lens, shape=(4, 4, 1, d))
+    got = run_attn(pages, q, tables, starts, held)
+    check_attn(pages, q, tables, starts, held, got)
+    flat = q.transpose(0, 2).contiguous().cuda()                       # [1, heads, n, d]
+    assert torch.equal(run_attn(pages, flat, tables, starts, held).transpose(0, 2), got)
+    major = torch.empty(1, 4, 4, d + 8, dtype=dtype, device="cuda")[..., :d].transpose(1, 2)
+    major.copy_(flat)
+    out = torch.full((1, 6, 4, d + 16), 3.0, dtype=dtype, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run_attn(pages, major, tables, starts, held, o=out[:, :4, :, :d].transpose(1, 2))
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out[:, :4, :, :d].transpose(1, 2), got.transpose(0, 2))
+    assert (out[..., d:] == 3).all() and (out[:, 4:] == 3).all()
+    more = torch.cat((flat, flat), 2)                                  # as many rows again that no request has
+    ws = lb.pages_workspace(pages, 4, 8, 2, 130)
+    o = torch.full_like(more, 3.0)
+    lb.lococo_pages_attn(pages, more, o, tables.cuda(), starts.cuda(), held.cuda(), 2, 130, ws)
+    assert torch.equal(o[:, :, :4], got.transpose(0, 2)) and (o[:, :, 4:] == 3).all()
+    pages.c.attn_scale = 0.375
+    check_attn(pages, q, tables, starts, held, run_attn(pages, q, tables, starts, held), scale=0.375)
+
+
+def test_attention_repeats_bit_for_bit():
+    batch = make_batch(61, torch.bfloat16, 2, 4, 128, 64, [(5000, 1), (300, 1), (2222, 1)])
+    first = run_attn(*batch)
+    for _ in range(3):
+        assert torch.equal(run_attn(*batch), first)
+
+
+def test_pages_beyond_32_bits():
+    """Codes of more than 4 GiB: rows in the first and the last pages."""
+    kv, d, R, P = 32, 128, 64, 34000                                   # 128 KiB of codes a page: 4.15 GiB
+    dtype = torch.bfloat16
+    pages = lb.Pages(dtype=dtype, n_q_heads=kv, n_kv_heads=kv, head_dim=d, page_rows=R, n_pages=P)
+    n = 3 * R - 5
+    k, v = (torch.randn(1, kv, n, d, generator=torch.Generator().manual_seed(s)).to(dtype) for s in (1, 2))
+    ids = torch.tensor([P - 1, 0, P - 2])
+    slots = (ids[torch.arange(n) // R] * R + torch.arange(n) % R).int()
+    lb.lococo_pages_store(pages, k.cuda(), v.cuda(), slots.cuda())
+    ko, vo = torch.empty_like(k, device="cuda"), torch.empty_like(v, device="cuda")
+    lb.lococo_pages_load(pages, slots.cuda(), ko, vo)
+    assert torch.equal(ko.cpu().double(), pu.values(*pu.four_bits(k))) and torch.equal(vo.cpu().double(), pu.values(*pu.four_bits(v)))
+    small = lb.Pages(dtype=dtype, n_q_heads=kv, n_kv_heads=kv, head_dim=d, page_rows=R, n_pages=3)
+    near = (torch.arange(n) // R * R + torch.arange(n) % R).int().cuda()
+    lb.lococo_pages_store(small, k.cuda(), v.cuda(), near)
+    for new in (1, 30):
+        q = torch.randn(1, kv, new, d).to(dtype)
+        starts, held = torch.tensor([0, new], dtype=torch.int32), torch.tensor([n], dtype=torch.int32)
+        far = run_attn(pages, q, ids[None].int(), starts, held)
+        assert torch.equal(far, run_attn(small, q, torch.arange(3).int()[None], starts, held))
+
+
+# ---- refusals
+def test_refusals():
+    kw = dict(dtype=torch.bfloat16, n_q_heads=4, n_kv_heads=2, head_dim=64, page_rows=16, n_pages=4)
+    pages, q, tables, starts, held = make_batch(71, torch.bfloat16, 2, 2, 64, 16, [(40, 2), (9, 1)])
+    q, o = q.cuda(), torch.full_like(q, 5.0, device="cuda")
+
+    def attn(p=pages, q=q, o=o, max_new=2, ws=lb.pages_workspace(pages, 2, 3, 2, 40)):
+        lb.lococo_pages_attn(p, q, o, tables.cuda(), starts.cuda(), held.cuda(), max_new, 40, ws)
+
+    def status(f, *a, **k):
+        with pytest.raises(lb.LococoError) as e:
+            f(*a, **k)
+        return e.value.status
+
+    for over, want in ((dict(head_dim=48), lb.LOCOCO_EUNSUPPORTED), (dict(head_dim=288), lb.LOCOCO_EUNSUPPORTED),
+                       (dict(page_rows=24), lb.LOCOCO_EUNSUPPORTED), (dict(page_rows=8), lb.LOCOCO_EUNSUPPORTED),
+                       (dict(page_rows=2048), lb.LOCOCO_EUNSUPPORTED), (dict(n_q_heads=5), lb.LOCOCO_EINVAL),
+                       (dict(n_q_heads=0), lb.LOCOCO_EINVAL), (dict(attn_scale=-1.0), lb.LOCOCO_EINVAL),
+                       (dict(attn_scale=math.nan), lb.LOCOCO_EINVAL)):
+        p = lb.Pages(**kw)
+        for f, x in over.items():
+            setattr(p.c, f, x)
+        assert status(lb.lococo_pages_workspace_bytes, p, 1, 1, 1, 16) == want, over
+    p = lb.Pages(**kw)
+    p.c.n_pages = 2 ** 27
+    assert status(lb.lococo_pages_workspace_bytes, p, 1, 1, 1, 16) == lb.LOCOCO_EUNSUPPORTED
+    p = lb.Pages(**kw)
+    p.c.v_codes = p.c.k_codes
+    assert status(lb.lococo_pages_workspace_bytes, p, 1, 1, 1, 16) == lb.LOCOCO_EINVAL
+    p = lb.Pages(**kw)
+    p.c.k_codes += 8
+    assert status(lb.lococo_pages_workspace_bytes, p, 1, 1, 1, 16) == lb.LOCOCO_EINVAL
+    assert status(lb.lococo_pages_workspace_bytes, pages, 5000, 1, 1, 16) == lb.LOCOCO_EUNSUPPORTED
+    assert status(attn, o=q) == lb.LOCOCO_EINVAL
+    assert status(attn, max_new=1) == lb.LOCOCO_EINVAL
+    shifted = torch.empty(q.numel() + 8, dtype=q.dtype, device="cuda")[4:4 + q.numel()].view(q.shape)
+    assert status(attn, q=shifted) == lb.LOCOCO_EINVAL
+    assert status(lb.lococo_pages_load, pages, torch.zeros(3, **I32), o[:, :2], o[:, :2]) == lb.LOCOCO_EINVAL
+    assert (o == 5).all()
+    e2 = torch.zeros(2, dtype=torch.int64, device="cuda")
+    ring, ends = pages.fresh_ring()
+    a = [torch.zeros(m, **I32) for m in (2, 2, 2, 3, 4, 4, 4)]
+    new, h, after, st, slots, pos, totals = a
+    t = tables.cuda()
+    assert status(lb.lococo_pages_plan, pages, new, h, t, ring, ends, h, e2, st, slots, pos, totals) == lb.LOCOCO_EINVAL
+    assert status(lb.lococo_pages_plan, pages, new, h, t, ring, ends, after, ends, st, slots, pos, totals) == lb.LOCOCO_EINVAL
+    many = torch.zeros(5000, **I32)
+    assert status(lb.lococo_pages_plan, pages, many, many.clone(), torch.zeros(5000, 3, **I32), ring, ends, many.clone(), e2,
+                  torch.zeros(5001, **I32), slots, pos, totals) == lb.LOCOCO_EUNSUPPORTED
