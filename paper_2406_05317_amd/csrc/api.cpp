@@ -1912,6 +1912,7 @@ lococo_status lococo_pages_attn(const lococo_pages* pages, const lococo_requests
   PagesAttnArgs a = pages_attn_args(pages, requests);
   a.q = rows_view(q, rows_per_batch);
   a.o = rows_view(o, rows_per_batch);
+  a.max_held = (int32_t)std::min<int64_t>(a.max_held, (int64_t)a.table_pages * pages->page_rows);
   const size_t need = align_up(pages_attn_workspace_bytes(pages->dtype, a), 256);
   if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
     return fail(LOCOCO_EWORKSPACE, "attention over pages needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,

@@ -1,15 +1,12 @@
 // Attention over paged 4-bit rows: o = softmax(scale q K^T) V for the new rows of a batch of requests of different lengths.
+#include "mfma_util.h"
 #include "pages.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lococo {
 namespace {
-
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // the request a token of the call belongs to: the last one that begins at or before it
 __device__ __forceinline__ int request_of(const int32_t* starts, int n, int32_t x) {
@@ -117,11 +114,483 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
   }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------------------
+// head_dim 64 and 128: matrix instructions.  A workgroup takes kRows = 16 QB query rows that share a kv head (the new rows of a request
+// times the heads of the group) and a part of the keys; its four waves take the 64-key tiles of that part in turn, each for all the
+// query rows with a running softmax of its own, and meet once, at the end.  No wave waits for another before that, nothing passes
+// through LDS on the way: codes go from memory to operand registers.
+//
+//   scores, transposed: S^T [64 keys x 16 queries] = K Q^T.  Lane (m = l % 16, g = l / 16) loads the codes of keys 4 m + t, t = 0 .. 3,
+//     columns g D/4 .. + D/4 - 1, which as bf16 (the conversion applies the scale; scale times code is exact in bf16) are the operand of
+//     key 4 m + t in MFMA t; the query operands take the columns in the same order.  The result has in lane (query l % 16, g) the keys
+//     16 g + 4 i + t: 16 consecutive ones.
+//   so the probabilities are where the second product, O^T = V^T P^T, wants them: lane (query, g) holds keys 16 g + 8 c + 0 .. 7 of
+//     step c.  Its other operand, V^T, wants in lane (column, g) those keys' values of one column: lane (m, g) loads, for its 16 keys,
+//     the D/32 bytes of columns D/16 m .. + D/16 - 1 and pairs two keys' values of a column after the conversion.
+//
+// Running softmax: the reference a row's exponentials are taken against moves only when a tile's largest score passes it by 8 (in powers
+// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits; one alone is off
+// by as much as the rounding of a bf16 result, where few keys carry a row by more than a test of that rounding allows), for fp32 rows of
+// three (all 24 bits), as their queries do.  Their sum is taken of the same numbers, by a product with ones: no vector instruction adds.
+constexpr int kTileWaves = 4, kTileKeys = 64;
+constexpr float kNoRef = -3.0e38f;             // below any score
+
+typedef __attribute__((ext_vector_type(4))) float f4;
+
+struct TileArgs {
+  PagesAttnArgs a;
+  int32_t splits, chunk;                       // parts of the keys at most, keys of a part at least
+  int32_t slots;                               // row tiles at most
+  int32_t by_request;                          // 1: a tile to a request
+  float* part_o;                               // [slot][kv head][part][row][D]
+  float* part_ml;                              // the same rows: reference, sum
+};
+
+// What a workgroup works on.  Row r of a request is query head r % group of its new row r / group.
+struct TileJob {
+  int32_t req, row0, rows, first, fresh, held; // rows of the tile; the request's first row of the call, its new rows, rows held
+  int32_t keys;                                // keys its last row sees
+};
+
+template <int TR>
+__device__ __forceinline__ bool tile_job(const TileArgs& g, int32_t slot, TileJob* j) {
+  const PagesAttnArgs& a = g.a;
+  int32_t req = slot, tile = 0;
+  if (!g.by_request) {
+    // request i's tiles begin at slot starts[i] * group / TR + i: with that a request's tiles never reach into the next one's
+    int lo = 0, hi = a.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((int32_t)((int64_t)a.starts[mid] * a.pg.group / TR) + mid <= slot) lo = mid; else hi = mid;
+    }
+    req = lo;
+    tile = slot - (int32_t)((int64_t)a.starts[req] * a.pg.group / TR) - req;
+    if (tile < 0) return false;
+  }
+  j->req = req;
+  j->first = min(max(a.starts[req], 0), a.tokens);
+  j->fresh = min(max(a.starts[req + 1], j->first), a.tokens) - j->first;
+  j->row0 = tile * TR;
+  const int64_t left = (int64_t)j->fresh * a.pg.group - (int64_t)tile * TR;
+  if (left <= 0) return false;
+  j->rows = (int32_t)min(left, (int64_t)TR);
+  j->held = min(max(a.held[req], 0), a.table_pages << a.pg.page_shift);
+  j->keys = max(j->held - j->fresh + (j->row0 + j->rows - 1) / a.pg.group + 1, 0);
+  return true;
+}
+// keys of a part, and how many parts there are (one at least): all from what the join knows as well
+__device__ __forceinline__ int32_t part_keys(const TileArgs& g, int32_t keys) {
+  const int32_t even = ((keys + g.splits - 1) / g.splits + kTileKeys - 1) / kTileKeys * kTileKeys;
+  return max(even, g.chunk);
+}
+__device__ __forceinline__ int32_t parts_of(const TileArgs& g, int32_t keys) {
+  return max((keys + part_keys(g, keys) - 1) / part_keys(g, keys), 1);
+}
+
+template <int BYTES>
+struct Bytes;
+template <>
+struct Bytes<16> { typedef u32x4 type; };
+template <>
+struct Bytes<8> { typedef u32x2 type; };
+template <>
+struct Bytes<4> { typedef uint32_t type; };
+template <>
+struct Bytes<2> { typedef uint16_t type; };
+
+// the codes and scales of a tile, as a lane holds them
+template <int D>
+struct TileCodes {
+  typename Bytes<D / 8>::type k[4];            // keys 4 m + t
+  uint32_t ks;                                 // their scales, a byte each
+  typename Bytes<D / 32>::type v[16];          // keys 16 g + x
+  u32x4 vs;
+};
+
+// key t's bf16 operand of a step: 8 values
+template <int D>
+__device__ __forceinline__ bf16x8 k_operand(const TileCodes<D>& c, int t, int step, float scale) {
+  const uint32_t w = c.k[t][step];
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  return __builtin_bit_cast(bf16x8, r);
+}
+template <int B>
+__device__ __forceinline__ uint32_t v_pair(uint32_t code, float scale) {      // columns 2 B, 2 B + 1 of a key
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, B));
+}
+__device__ __forceinline__ float scale_byte(uint32_t w, int i) { return __uint_as_float((i < 3 ? w << (23 - 8 * i) : w >> 1) & 0x7f800000u); }
+
+__device__ __forceinline__ f4 mfma16(bf16x8 a, bf16x8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// the largest over the four lanes that hold a query's keys
+__device__ __forceinline__ float max_groups(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return max_halves(x);
+}
+
+// the page of a key as a lane needs it: -1 where there is none
+__device__ __forceinline__ int32_t page_of(const PagesAttnArgs& a, const int32_t* table, int32_t key, int32_t held) {
+  const int32_t page = key < held ? table[key >> a.pg.page_shift] : -1;
+  return (uint32_t)page < (uint32_t)a.pg.n_pages ? page : -1;
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t kpage, int32_t vpage, int m,
+                                          int g) {
+  const int32_t krow = (key0 + 4 * m) & (pg.page_rows - 1), vrow = (key0 + 16 * g) & (pg.page_rows - 1);
+  const int64_t kat = ((int64_t)max(kpage, 0) * pg.Hkv + kvh) * pg.page_rows, vat = ((int64_t)max(vpage, 0) * pg.Hkv + kvh) * pg.page_rows;
+  const uint8_t* kc = pg.k_codes + (kat + krow) * (D / 2) + g * (D / 8);
+  const uint8_t* vc = pg.v_codes + (vat + vrow) * (D / 2) + m * (D / 32);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) c.k[t] = *(const typename Bytes<D / 8>::type*)(kc + t * (D / 2));
+  c.ks = *(const uint32_t*)(pg.k_scales + kat * (D / 32) + (g * (D / 4) / 32) * pg.page_rows + krow);
+#pragma unroll
+  for (int x = 0; x < 16; ++x) c.v[x] = *(const typename Bytes<D / 32>::type*)(vc + x * (D / 2));
+  c.vs = *(const u32x4*)(pg.v_scales + vat * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + vrow);
+}
+
+template <typename T, int D, int QB>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs g) {
+  constexpr int PARTS = std::is_same<T, float>::value ? 3 : 1, PROBS = PARTS == 3 ? 3 : 2, TR = 16 * QB, STEPS = D / 32, COLS = D / 16, LD = D + 4;
+  __shared__ __align__(16) float joined[kTileWaves][TR][LD];
+  __shared__ float ml[kTileWaves][TR][2];
+  __shared__ int32_t nan_key[D / 32];          // first visible key whose 32 values of V stand for NaN, among the tiles that mask
+  const PagesAttnArgs& a = g.a;
+  const PagesView& pg = a.pg;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, m = l & 15, grp = l >> 4;
+  const int item = xcd_item(blockIdx.x, gridDim.x);
+  const int32_t slot = item % g.slots, split = item / g.slots % g.splits, kvh = item / g.slots / g.splits;
+  TileJob job;
+  if (!tile_job<TR>(g, slot, &job)) return;
+  const int32_t per = part_keys(g, job.keys), parts = parts_of(g, job.keys);
+  if (split >= parts) return;
+  const int32_t key_lo = split * per, key_hi = min(key_lo + per, job.keys);
+  if (threadIdx.x < D / 32) nan_key[threadIdx.x] = 0x7fffffff;
+  __syncthreads();
+
+  // queries: row 16 qb + m, columns grp D/4 + 8 step ..
+  bf16x8 q[QB][PARTS][STEPS];
+  int32_t last[QB];                            // the key a row's query stands at
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int32_t r = 16 * qb + m, row = job.row0 + r;
+    const bool real = r < job.rows;
+    const int32_t x = row / pg.group, token = job.first + x, b = token / a.q.t, t = token - b * a.q.t;
+    last[qb] = real ? job.held - job.fresh + x : -1;
+    const T* qr = (const T*)a.q.p + (real ? b * a.q.sb + (kvh * pg.group + row - x * pg.group) * a.q.sh + t * a.q.st : 0) + grp * (D / 4);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if constexpr (PARTS == 1) {
+        u32x4 v = {0, 0, 0, 0};
+        if (real) v = *(const u32x4*)(qr + 8 * s);
+        q[qb][0][s] = __builtin_bit_cast(bf16x8, v);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = real ? (float)qr[8 * s + i] : 0.f;
+        bf16x8 part[PARTS];
+        split_parts<PARTS>(v, part);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) q[qb][p][s] = part[p];
+      }
+    }
+  }
+  const float c = pg.scale * kLog2e;
+  const int32_t whole = job.held - job.fresh + job.row0 / pg.group + 1;       // keys every row of the tile sees
+  const int32_t* table = a.tables + (int64_t)job.req * a.table_pages;
+  float ref[QB];
+  f4 o[QB][COLS], sum[QB];                     // sum: the same number in all four places of a lane
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    ref[qb] = kNoRef;
+    sum[qb] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) o[qb][j] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  constexpr int kStride = kTileWaves * kTileKeys;
+  int32_t key0 = key_lo + w * kTileKeys;
+  int32_t kp = page_of(a, table, key0 + 4 * m, key_hi), vp = page_of(a, table, key0 + 16 * grp, key_hi);
+  TileCodes<D> cur;
+  if (key0 < key_hi) load_tile<D>(cur, pg, kvh, key0, kp, vp, m, grp);
+  int32_t kp1 = page_of(a, table, key0 + kStride + 4 * m, key_hi), vp1 = page_of(a, table, key0 + kStride + 16 * grp, key_hi);
+  while (key0 < key_hi) {
+    TileCodes<D> nxt;
+    const int32_t key1 = key0 + kStride;
+    const bool more = key1 < key_hi;
+    if (more) load_tile<D>(nxt, pg, kvh, key1, kp1, vp1, m, grp);
+    const int32_t kp2 = page_of(a, table, key1 + kStride + 4 * m, key_hi), vp2 = page_of(a, table, key1 + kStride + 16 * grp, key_hi);
+
+    f4 s[QB][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const float sc = scale_byte(cur.ks, t);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) s[qb][t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const bf16x8 k = k_operand<D>(cur, t, st, sc);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) s[qb][t] = mfma16(k, q[qb][p][st], s[qb][t]);
+      }
+    }
+    u32x4 vs = cur.vs;
+    if (key0 + kTileKeys > min(whole, key_hi) || __any(vp < 0)) {
+      // keys behind a row's own, behind the part, or without a page: no score, and a V that is zero times something finite.  A key that
+      // only some rows see may stand for NaN: taken out of the product here and put into those rows at the end.
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const int32_t lim = vp < 0 ? -1 : min(last[qb], key_hi - 1);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[qb][t][i] = key0 + 16 * grp + 4 * i + t <= lim ? s[qb][t][i] : -INFINITY;
+      }
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int32_t key = key0 + 16 * grp + x;
+        const bool in = vp >= 0 && key < key_hi, odd = (vs[x / 4] >> (8 * (x % 4)) & 255u) == 255u;
+        if (in && odd) atomicMin(&nan_key[m * (D / 16) / 32], key);
+        if (!in || odd) vs[x / 4] &= ~(255u << (8 * (x % 4)));
+      }
+    }
+    bf16x8 p[QB][PROBS][2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float top = s[qb][0][0];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[qb][t][i]);
+      top *= c;
+      if (__any(top > ref[qb] + 8.f)) {
+        const float next = fmaxf(ref[qb], max_groups(top)), keep = __builtin_amdgcn_exp2f(ref[qb] - next);
+        ref[qb] = next;
+        sum[qb] = f4{sum[qb][0] * keep, sum[qb][1] * keep, sum[qb][2] * keep, sum[qb][3] * keep};
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) o[qb][j] = f4{o[qb][j][0] * keep, o[qb][j][1] * keep, o[qb][j][2] * keep, o[qb][j][3] * keep};
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float e[8];                             // keys 16 grp + 8 h + 4 i + t
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) e[4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
+        bf16x8 part[PROBS];
+        split_parts<PROBS>(e, part);
+#pragma unroll
+        for (int k = PROBS - 1; k >= 0; --k) {
+          p[qb][k][h] = part[k];
+          sum[qb] = mfma16(ones, part[k], sum[qb]);
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float sc[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) sc[x] = scale_byte(vs[2 * h + x / 4], x % 4);
+      auto columns = [&](auto byte) {
+        constexpr int B = decltype(byte)::value;
+        uint32_t y[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] = v_pair<B>(cur.v[8 * h + x], sc[x]);
+        u32x4 even, odd;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          even[x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x05040100u);
+          odd[x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x07060302u);
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int k = PROBS - 1; k >= 0; --k) {
+            o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][k][h], o[qb][2 * B]);
+            o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][k][h], o[qb][2 * B + 1]);
+          }
+      };
+      columns(std::integral_constant<int, 0>());
+      columns(std::integral_constant<int, 1>());
+      if constexpr (D == 128) {
+        columns(std::integral_constant<int, 2>());
+        columns(std::integral_constant<int, 3>());
+      }
+    }
+    cur = nxt;
+    key0 = key1;
+    kp = kp1;
+    vp = vp1;
+    kp1 = kp2;
+    vp1 = vp2;
+  }
+
+  // the four waves' results to one: o[qb][j][i] is column COLS (4 grp + i) + j of row 16 qb + m
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    if (grp == 0) {
+      ml[w][16 * qb + m][0] = ref[qb];
+      ml[w][16 * qb + m][1] = sum[qb][0];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < COLS; j += 4)
+        *(f4*)&joined[w][16 * qb + m][COLS * (4 * grp + i) + j] = f4{o[qb][j][i], o[qb][j + 1][i], o[qb][j + 2][i], o[qb][j + 3][i]};
+  }
+  __syncthreads();
+  constexpr int PER = TR * D / (64 * kTileWaves);                             // columns of a thread
+  const int r = threadIdx.x / (D / PER), col = threadIdx.x % (D / PER) * PER;
+  if (r >= job.rows) return;
+  float best = ml[0][r][0];
+#pragma unroll
+  for (int k = 1; k < kTileWaves; ++k) best = fmaxf(best, ml[k][r][0]);
+  float y[PER], total = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) y[i] = 0.f;
+#pragma unroll
+  for (int k = 0; k < kTileWaves; ++k) {
+    const float keep = __builtin_amdgcn_exp2f(ml[k][r][0] - best);
+    total += ml[k][r][1] * keep;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) y[i] += joined[k][r][col + i] * keep;
+  }
+  const int32_t row = job.row0 + r, x = row / pg.group, at = job.held - job.fresh + x;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (at >= nan_key[(col + i) / 32]) y[i] = NAN;
+  if (parts > 1) {
+    const int64_t pr = (((int64_t)slot * pg.Hkv + kvh) * g.splits + split) * TR + r;
+#pragma unroll
+    for (int i = 0; i < PER; i += 4) *(f4*)(g.part_o + pr * D + col + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    if (col == 0) {
+      g.part_ml[2 * pr] = best;
+      g.part_ml[2 * pr + 1] = total;
+    }
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;                         // a row that sees nothing: zeros
+  const int32_t token = job.first + x, ob = token / a.o.t, ot = token - ob * a.o.t;
+  T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st + col;
+  __align__(16) T z[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) z[i] = (T)(y[i] * inv);
+  if constexpr (PARTS == 1) {
+    constexpr int V = PER * 2 < 16 ? PER * 2 : 16;
+#pragma unroll
+    for (int i = 0; i < PER * 2 / V; ++i) ((typename Bytes<V>::type*)out)[i] = ((typename Bytes<V>::type*)z)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) out[i] = z[i];
+  }
+}
+
+// The parts of a row to one, in their order: a workgroup to a row, its waves the parts in turn.
+template <typename T, int D, int TR>
+__global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t rows) {
+  __shared__ float sums[4][D], stat[4][2];
+  const PagesAttnArgs& a = g.a;
+  const PagesView& pg = a.pg;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int32_t r = blockIdx.x % rows, kvh = blockIdx.x / rows % pg.Hkv, slot = blockIdx.x / rows / pg.Hkv;
+  TileJob job;
+  if (!tile_job<TR>(g, slot, &job) || r >= job.rows) return;
+  const int32_t parts = parts_of(g, job.keys);
+  if (parts == 1) return;
+  const int64_t pr = ((int64_t)slot * pg.Hkv + kvh) * g.splits * TR + r;
+  float best = kNoRef, total = 0.f, y[D / 64];
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) y[i] = 0.f;
+  for (int32_t k = w; k < parts; k += 4) {
+    const float pm = g.part_ml[2 * (pr + (int64_t)k * TR)], pl = g.part_ml[2 * (pr + (int64_t)k * TR) + 1];
+    const float next = fmaxf(best, pm), keep = __builtin_amdgcn_exp2f(best - next), f = __builtin_amdgcn_exp2f(pm - next);
+    best = next;
+    total = total * keep + pl * f;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) y[i] = y[i] * keep + g.part_o[(pr + (int64_t)k * TR) * D + l + 64 * i] * f;
+  }
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) sums[w][l + 64 * i] = y[i];
+  if (l == 0) {
+    stat[w][0] = best;
+    stat[w][1] = total;
+  }
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  best = fmaxf(fmaxf(stat[0][0], stat[1][0]), fmaxf(stat[2][0], stat[3][0]));
+  total = 0.f;
+  float z = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float f = __builtin_amdgcn_exp2f(stat[k][0] - best);
+    total += stat[k][1] * f;
+    z += sums[k][threadIdx.x] * f;
+  }
+  const int32_t row = job.row0 + r, x = row / pg.group, token = job.first + x, ob = token / a.o.t, ot = token - ob * a.o.t;
+  T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st;
+  out[threadIdx.x] = (T)(total == 0.f ? 0.f : z / total);
+}
+
+bool tile_fits(int d) { return d == 64 || d == 128; }
+
+// How the work is dealt out.  Row tiles of 32 where a request has more than 16 rows (new rows times the group) and rows are bf16.
+// Parts of the keys: as many as bring the launch to about kTileTarget workgroups, a part of 256 keys at least (one tile a wave).
+constexpr int kTileTarget = 1024;
+struct TilePlan { int qb, rows, slots, splits, chunk, by_request; size_t rows_all; };
+TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
+  TilePlan p{};
+  const int64_t most = (int64_t)a.max_new * a.pg.group;
+  p.qb = dtype == LOCOCO_BF16 && most > 16 ? 2 : 1;
+  const int tr = 16 * p.qb;
+  p.by_request = most <= tr;
+  p.rows = (int)(most < tr ? most : tr);
+  p.slots = p.by_request ? a.n : (int)((int64_t)a.tokens * a.pg.group / tr) + a.n;
+  // tiles that have rows, about
+  const int64_t units = (p.by_request ? a.n : ((int64_t)a.tokens * a.pg.group + tr - 1) / tr) * a.pg.Hkv;
+  const int64_t keys = a.max_held > 0 ? a.max_held : 1;
+  constexpr int64_t kLeast = kTileWaves * kTileKeys;
+  // not fewer parts for more keys: a workspace for many takes fewer
+  const int64_t want = std::max<int64_t>(kTileTarget / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
+  p.splits = (int)splits;
+  p.chunk = (int)std::max<int64_t>(kLeast, ((keys + splits - 1) / splits + kTileKeys - 1) / kTileKeys * kTileKeys);
+  p.rows_all = (size_t)p.slots * a.pg.Hkv * p.splits * tr;
+  return p;
+}
+
+template <typename T, int D, int QB>
+hipError_t launch_tile(const TileArgs& g, const TilePlan& p, hipStream_t s) {
+  const unsigned grid = (unsigned)p.slots * (unsigned)p.splits * (unsigned)g.a.pg.Hkv;
+  pages_attn_tile_k<T, D, QB><<<grid, 64 * kTileWaves, 0, s>>>(g);
+  if (p.splits > 1)
+    pages_attn_join_k<T, D, 16 * QB><<<(unsigned)p.slots * (unsigned)g.a.pg.Hkv * (unsigned)p.rows, 256, 0, s>>>(g, p.rows);
+  return hipGetLastError();
+}
+
 }  // namespace
 
-size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a) { return 0; }
+size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a) {
+  if (!tile_fits(a.pg.d)) return 0;
+  const TilePlan p = tile_plan(dtype, a);
+  return p.splits > 1 ? p.rows_all * (a.pg.d + 2) * sizeof(float) : 0;
+}
 
 hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace, hipStream_t s) {
+  if (tile_fits(a.pg.d)) {
+    const TilePlan p = tile_plan(dtype, a);
+    TileArgs g{a, p.splits, p.chunk, p.slots, p.by_request, (float*)workspace, (float*)workspace + p.rows_all * a.pg.d};
+    if (dtype == LOCOCO_F32) return a.pg.d == 64 ? launch_tile<float, 64, 1>(g, p, s) : launch_tile<float, 128, 1>(g, p, s);
+    if (p.qb == 1) return a.pg.d == 64 ? launch_tile<__bf16, 64, 1>(g, p, s) : launch_tile<__bf16, 128, 1>(g, p, s);
+    return a.pg.d == 64 ? launch_tile<__bf16, 64, 2>(g, p, s) : launch_tile<__bf16, 128, 2>(g, p, s);
+  }
   const dim3 grid((unsigned)((a.tokens + kRowsWaves - 1) / kRowsWaves), (unsigned)a.pg.Hq);
   if (dtype == LOCOCO_F32) pages_attn_rows_k<float><<<grid, 64 * kRowsWaves, 0, s>>>(a);
   else pages_attn_rows_k<__bf16><<<grid, 64 * kRowsWaves, 0, s>>>(a);
