@@ -258,7 +258,7 @@ class Pages:
         self.c = lococo_pages(C.sizeof(lococo_pages), _dtype_code(dtype), n_q_heads, n_kv_heads, head_dim, page_rows, n_pages,
                               attn_scale, self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
                               self.v_scales.data_ptr())
-        self.dtype, self.device = dtype, device
+        self.ref, self.dtype, self.device = C.byref(self.c), dtype, device
 
     def fresh_ring(self):
         """(ring, ends) with every page free, as lococo_pages_plan takes them."""
@@ -373,60 +373,82 @@ def lococo_sequence_backward(cfg, q, k, v, B: int, conv_w, conv_b, cache: Cache,
         _ptr(d_conv_b), _ptr(workspace), ws_bytes, _stream()))
 
 
-def _numbers(dtype, **arrays):
-    for name, t in arrays.items():
-        assert t.dtype == dtype and t.is_contiguous() and t.is_cuda, f"{name}: expected contiguous {dtype} on the device"
+# The calls on pages are short enough for the marshalling to count: their checks and addresses are taken in one go.
+_I32, _I64 = torch.int32, torch.int64
+
+
+def _numbers(dtype, *arrays):
+    """Addresses of contiguous device arrays of whole numbers."""
+    for t in arrays:
+        if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"expected a contiguous {dtype} array on the device, got {t.dtype}, {t.device}, strides {t.stride()}")
+    return [t.data_ptr() for t in arrays]
+
+
+def _rows(pages: Pages, t: torch.Tensor, heads: int) -> lococo_tensor:
+    """View of a [b, heads, t, d] tensor of the pages' type."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not pages.dtype or not t.is_cuda or len(shape) != 4 or shape[1] != heads or shape[3] != pages.c.head_dim or stride[3] != 1:
+        raise TypeError(f"expected [b, {heads}, t, {pages.c.head_dim}] of {pages.dtype} on the device with the last axis contiguous, got "
+                        f"{tuple(shape)} of {t.dtype}, {t.device}, strides {stride}")
+    return lococo_tensor(t.data_ptr(), stride[0], stride[1], stride[2])
+
+
+def _stream_now() -> int:
+    """The current device's current stream: as _stream(), without an object for it."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def lococo_pages_plan(pages: Pages, new_rows, held, tables, ring, ends, held_after, ends_after, starts, slots, positions, totals):
     """Pages, slots and positions of a turn from its requests' lengths (all arrays on the device: int32, ends int64)."""
-    _numbers(torch.int32, new_rows=new_rows, held=held, tables=tables, ring=ring, held_after=held_after, starts=starts, slots=slots,
-             positions=positions, totals=totals)
-    _numbers(torch.int64, ends=ends, ends_after=ends_after)
+    new_p, held_p, tables_p, ring_p, after_p, starts_p, slots_p, positions_p, totals_p = _numbers(
+        _I32, new_rows, held, tables, ring, held_after, starts, slots, positions, totals)
+    ends_p, ends_after_p = _numbers(_I64, ends, ends_after)
     n, width = tables.shape
-    assert new_rows.numel() == held.numel() == held_after.numel() == n and starts.numel() == n + 1
-    assert ring.numel() == pages.c.n_pages and ends.numel() == ends_after.numel() == 2
-    assert slots.numel() == positions.numel() and totals.numel() == 4
-    _check(lib().lococo_pages_plan(C.byref(pages.c), n, slots.numel(), width, *(_ptr(t) for t in (
-        new_rows, held, tables, ring, ends, held_after, ends_after, starts, slots, positions, totals)), _stream()))
+    tokens = slots.numel()
+    if not (new_rows.numel() == held.numel() == held_after.numel() == starts.numel() - 1 == n and positions.numel() == tokens and
+            ring.numel() == pages.c.n_pages and ends.numel() == ends_after.numel() == 2 and totals.numel() == 4):
+        raise ValueError("arrays of the plan do not fit each other")
+    _check(lib().lococo_pages_plan(pages.ref, n, tokens, width, new_p, held_p, tables_p, ring_p, ends_p, after_p, ends_after_p, starts_p,
+                                   slots_p, positions_p, totals_p, _stream_now()))
 
 
-def _rows(pages: Pages, t: torch.Tensor, heads: int) -> lococo_tensor:
-    assert t.dtype == pages.dtype and t.is_cuda and t.shape[1] == heads and t.shape[3] == pages.c.head_dim
-    return _tensor(t)
+def _slots_of(slots, k, v):
+    if k.shape != v.shape or slots.numel() != k.shape[0] * k.shape[2]:
+        raise ValueError(f"{slots.numel()} slots for k, v of {tuple(k.shape)}, {tuple(v.shape)}")
+    return _numbers(_I32, slots)[0]
 
 
 def lococo_pages_store(pages: Pages, k, v, slots):
     """k, v [b, n_kv_heads, t, d] to 4 bits, row (b, t) at slots[b * T + t]."""
-    _numbers(torch.int32, slots=slots)
-    assert k.shape == v.shape and slots.numel() == k.shape[0] * k.shape[2]
     x, y = _rows(pages, k, pages.c.n_kv_heads), _rows(pages, v, pages.c.n_kv_heads)
-    _check(lib().lococo_pages_store(C.byref(pages.c), C.byref(x), C.byref(y), max(k.shape[2], 1), slots.numel(), _ptr(slots), _stream()))
+    at = _slots_of(slots, k, v)
+    _check(lib().lococo_pages_store(pages.ref, C.byref(x), C.byref(y), max(k.shape[2], 1), slots.numel(), at, _stream_now()))
 
 
 def lococo_pages_load(pages: Pages, slots, k, v):
     """The rows at `slots` into k, v [b, n_kv_heads, t, d]."""
-    _numbers(torch.int32, slots=slots)
-    assert k.shape == v.shape and slots.numel() == k.shape[0] * k.shape[2]
     x, y = _rows(pages, k, pages.c.n_kv_heads), _rows(pages, v, pages.c.n_kv_heads)
-    _check(lib().lococo_pages_load(C.byref(pages.c), _ptr(slots), max(k.shape[2], 1), slots.numel(), C.byref(x), C.byref(y), _stream()))
+    at = _slots_of(slots, k, v)
+    _check(lib().lococo_pages_load(pages.ref, at, max(k.shape[2], 1), slots.numel(), C.byref(x), C.byref(y), _stream_now()))
 
 
 def lococo_pages_workspace_bytes(pages: Pages, n: int, tokens: int, max_new: int, max_held: int, table_pages: int = 1) -> int:
     r, out = lococo_requests(n, tokens, table_pages, max_new, max_held, None, None, None), C.c_size_t(0)
-    _check(lib().lococo_pages_workspace_bytes(C.byref(pages.c), C.byref(r), C.byref(out)))
+    _check(lib().lococo_pages_workspace_bytes(pages.ref, C.byref(r), C.byref(out)))
     return out.value
 
 
 def lococo_pages_attn(pages: Pages, q, o, tables, starts, held, max_new: int, max_held: int, workspace=None):
     """Attention of the requests' new rows q [b, n_q_heads, t, d] over all rows of their request, into o."""
-    _numbers(torch.int32, tables=tables, starts=starts, held=held)
-    n, width = tables.shape
-    assert q.shape == o.shape and starts.numel() == n + 1 and held.numel() == n
     x, y = _rows(pages, q, pages.c.n_q_heads), _rows(pages, o, pages.c.n_q_heads)
-    r = lococo_requests(n, q.shape[0] * q.shape[2], width, max_new, max_held, _ptr(tables), _ptr(starts), _ptr(held))
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().lococo_pages_attn(C.byref(pages.c), C.byref(r), C.byref(x), C.byref(y), max(q.shape[2], 1), _ptr(workspace), ws_bytes, _stream()))
+    n, width = tables.shape
+    b, _, t, _ = q.shape
+    if q.shape != o.shape or starts.numel() != n + 1 or held.numel() != n:
+        raise ValueError("o, starts or held do not fit q and the tables")
+    r = lococo_requests(n, b * t, width, max_new, max_held, *_numbers(_I32, tables, starts, held))
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().lococo_pages_attn(pages.ref, C.byref(r), C.byref(x), C.byref(y), max(t, 1), ws, ws_bytes, _stream_now()))
 
 
 def lococo_scan_status(cfg, workspace) -> int:

@@ -13,11 +13,11 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Plan.  Three running sums over the requests give every row's place: of the new rows (where a request's rows begin in the call), of
 // the pages needed (which of the free ones are whose) and of the pages given back.  Every workgroup computes them all, n numbers from
-// the L2, and places kPlanTokens rows: no workgroup waits for another, and one launch does.  What this call writes no part of it reads:
+// the L2, and places a share of the rows, one a lane where the device holds that many: no workgroup waits for another, and one launch does.  What this call writes no part of it reads:
 // a request's new table entries lie behind the ones it reads, what is given back goes to the ring behind its free part.
 // Sums saturate at kPagesCap (addition cut off at a bound is associative for numbers >= 0): lengths that make no sense stay sums that
 // refuse.  Bound by the launch and some three round trips to memory.
-constexpr int kPlanThreads = 256, kPlanTokens = 2048;
+constexpr int kPlanThreads = 256;
 
 __device__ __forceinline__ int32_t add_cap(int32_t a, int32_t b) { return min(a + b, kPagesCap); }
 
@@ -91,14 +91,13 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
   const int32_t avail = (int32_t)min(max(tail - head, (int64_t)0), (int64_t)a.n_pages);
   int32_t taken = 0, refused = 0, laid = 0;
   for (int i = i0; i < i1; ++i) {
-    const int32_t next = i + 1 < i1 ? start[i + 1] : -1, h = held[i];
+    const int32_t h = held[i];
     if (h < 0) {
       off[i] = give;
       give = add_cap(give, (-1 - h + R - 1) >> sh);
       continue;
     }
-    // the rows of the last request of this thread: read again (its neighbour may not have written its start yet)
-    const int32_t cnt = next >= 0 ? next - start[i] : min(max(a.new_rows[i], 0), kPagesCap);
+    const int32_t cnt = (i + 1 < n ? start[i + 1] : rows) - start[i];       // written ahead of the second sum's barriers
     const int32_t after = (h + cnt + R - 1) >> sh;
     const bool fits = add_cap(start[i], cnt) <= a.tokens && after <= a.table_pages;
     const int32_t need = fits ? after - ((h + R - 1) >> sh) : 0;
@@ -132,8 +131,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
     a.totals[3] = sums[2];
   }
   const int32_t P = a.n_pages, head_at = (int32_t)(((head % P) + P) % P), tail_at = (int32_t)(((tail % P) + P) % P);
-  const int32_t x1 = min((int64_t)a.tokens, (int64_t)(blockIdx.x + 1) * kPlanTokens);
-  for (int32_t x = blockIdx.x * kPlanTokens + tid; x < x1; x += kPlanThreads) {
+  for (int64_t x = blockIdx.x * kPlanThreads + tid; x < a.tokens; x += gridDim.x * kPlanThreads) {
     int32_t slot = -1, pos = -1;
     if (x < rows) {
       int lo = 0, hi = n;                        // the last request that begins at or before row x: requests without rows begin with
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
       }
       const int32_t h = held[lo], o = off[lo];
       if (h >= 0 && o >= 0) {
-        pos = h + x - start[lo];
+        pos = h + (int32_t)x - start[lo];
         const int32_t j = pos >> sh, had = (h + R - 1) >> sh;
         int32_t page;
         if (j < had) {
@@ -194,15 +192,13 @@ __device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
 
 template <typename T>
 __device__ __forceinline__ const T* row_of(const RowsView& r, int32_t token, int32_t head) {
-  const int32_t b = token / r.t, t = token - b * r.t;
+  const int32_t b = token < r.t ? 0 : token / r.t, t = token - b * r.t;
   return (const T*)r.p + b * r.sb + head * r.sh + t * r.st;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsView k, RowsView v, int32_t tokens, const int32_t* slots) {
-  const int per_row = pg.d / 8;                  // lanes to a row
-  const int64_t id = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-  const int32_t token = (int32_t)(id / per_row), c = (int32_t)(id % per_row), head = blockIdx.y;
+  const int32_t token = blockIdx.x * blockDim.y + threadIdx.y, c = threadIdx.x, head = blockIdx.y;
   if (token >= tokens) return;                   // the four lanes of a block leave together
   const int32_t slot = slots[token];
   const int32_t page = slot >> pg.page_shift, row = slot & (pg.page_rows - 1);
@@ -232,9 +228,7 @@ __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsV
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void pages_load_k(PagesView pg, RowsView k, RowsView v, int32_t tokens, const int32_t* slots) {
-  const int per_row = pg.d / 8;
-  const int64_t id = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-  const int32_t token = (int32_t)(id / per_row), c = (int32_t)(id % per_row), head = blockIdx.y;
+  const int32_t token = blockIdx.x * blockDim.y + threadIdx.y, c = threadIdx.x, head = blockIdx.y;
   if (token >= tokens) return;
   const int32_t slot = slots[token];
   const int32_t page = slot >> pg.page_shift, row = slot & (pg.page_rows - 1);
@@ -262,30 +256,33 @@ __global__ __launch_bounds__(kRowThreads) void pages_load_k(PagesView pg, RowsVi
   }
 }
 
+// lanes of a row along x, rows along y (a workgroup is a whole number of waves where head_dim is a power of two)
+dim3 row_block(const PagesView& pg) { return dim3((unsigned)(pg.d / 8), (unsigned)(kRowThreads / (pg.d / 8))); }
 dim3 row_grid(const PagesView& pg, int32_t tokens) {
-  const int64_t lanes = (int64_t)tokens * (pg.d / 8);
-  return dim3((unsigned)((lanes + kRowThreads - 1) / kRowThreads), (unsigned)pg.Hkv, 2);
+  const int rows = kRowThreads / (pg.d / 8);
+  return dim3((unsigned)((tokens + rows - 1) / rows), (unsigned)pg.Hkv, 2);
 }
 
 }  // namespace
 
 hipError_t launch_pages_plan(const PagesPlanArgs& a, hipStream_t s) {
-  const unsigned grid = a.tokens > 0 ? (unsigned)((a.tokens + kPlanTokens - 1) / kPlanTokens) : 1u;
+  const unsigned want = (unsigned)((a.tokens + kPlanThreads - 1) / kPlanThreads), most = 2u * (unsigned)cu_count();
+  const unsigned grid = want < 1 ? 1u : want < most ? want : most;
   pages_plan_k<<<grid, kPlanThreads, 3 * sizeof(int32_t) * (size_t)a.n, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_store(int dtype, const PagesView& pg, const RowsView& k, const RowsView& v, int32_t tokens,
                               const int32_t* slots, hipStream_t s) {
-  if (dtype == LOCOCO_F32) pages_store_k<float><<<row_grid(pg, tokens), kRowThreads, 0, s>>>(pg, k, v, tokens, slots);
-  else pages_store_k<__bf16><<<row_grid(pg, tokens), kRowThreads, 0, s>>>(pg, k, v, tokens, slots);
+  if (dtype == LOCOCO_F32) pages_store_k<float><<<row_grid(pg, tokens), row_block(pg), 0, s>>>(pg, k, v, tokens, slots);
+  else pages_store_k<__bf16><<<row_grid(pg, tokens), row_block(pg), 0, s>>>(pg, k, v, tokens, slots);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_load(int dtype, const PagesView& pg, const RowsView& k, const RowsView& v, int32_t tokens,
                              const int32_t* slots, hipStream_t s) {
-  if (dtype == LOCOCO_F32) pages_load_k<float><<<row_grid(pg, tokens), kRowThreads, 0, s>>>(pg, k, v, tokens, slots);
-  else pages_load_k<__bf16><<<row_grid(pg, tokens), kRowThreads, 0, s>>>(pg, k, v, tokens, slots);
+  if (dtype == LOCOCO_F32) pages_load_k<float><<<row_grid(pg, tokens), row_block(pg), 0, s>>>(pg, k, v, tokens, slots);
+  else pages_load_k<__bf16><<<row_grid(pg, tokens), row_block(pg), 0, s>>>(pg, k, v, tokens, slots);
   return hipGetLastError();
 }
 
