@@ -263,7 +263,11 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   const PagesView& pg = a.pg;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, m = l & 15, grp = l >> 4;
   const int item = xcd_item(blockIdx.x, gridDim.x);
-  const int32_t slot = item % g.slots, split = item / g.slots % g.splits, kvh = item / g.slots / g.splits;
+  // neighbours, on one XCD: the kv heads of a part where a request is one tile (their scales share cache lines), else the tiles that
+  // read the same keys
+  const int32_t kvh = g.by_request ? item % pg.Hkv : item / g.slots / g.splits;
+  const int32_t rest = g.by_request ? item / pg.Hkv : item % (g.slots * g.splits);
+  const int32_t slot = g.by_request ? rest / g.splits : rest % g.slots, split = g.by_request ? rest % g.splits : rest / g.slots;
   TileJob job;
   if (!tile_job<TR>(g, slot, &job)) return;
   const int32_t per = part_keys(g, job.keys), parts = parts_of(g, job.keys);
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   for (int qb = 0; qb < QB; ++qb) {
     const int32_t r = 16 * qb + m, row = job.row0 + r;
     const bool real = r < job.rows;
-    const int32_t x = row / pg.group, token = job.first + x, b = token / a.q.t, t = token - b * a.q.t;
+    const int32_t x = row / pg.group, token = job.first + x, b = token < a.q.t ? 0 : token / a.q.t, t = token - b * a.q.t;
     last[qb] = real ? job.held - job.fresh + x : -1;
     const T* qr = (const T*)a.q.p + (real ? b * a.q.sb + (kvh * pg.group + row - x * pg.group) * a.q.sh + t * a.q.st : 0) + grp * (D / 4);
 #pragma unroll
@@ -479,7 +483,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
     return;
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;                         // a row that sees nothing: zeros
-  const int32_t token = job.first + x, ob = token / a.o.t, ot = token - ob * a.o.t;
+  const int32_t token = job.first + x, ob = token < a.o.t ? 0 : token / a.o.t, ot = token - ob * a.o.t;
   T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st + col;
   __align__(16) T z[PER];
 #pragma unroll
@@ -494,57 +498,89 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   }
 }
 
-// The parts of a row to one, in their order: a workgroup to a row, its waves the parts in turn.
-template <typename T, int D, int TR>
+// The parts of a row to one, in their order.  WAVES waves to a row, which take its parts in turn: one where there are few, so that four
+// rows share a workgroup.  A lane holds the reference and the sum of one part, all lanes the columns of every part.
+template <typename T, int D, int TR, int WAVES>
 __global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t rows) {
+  typedef __attribute__((ext_vector_type(D / 64))) float cols;
   __shared__ float sums[4][D], stat[4][2];
   const PagesAttnArgs& a = g.a;
   const PagesView& pg = a.pg;
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int32_t r = blockIdx.x % rows, kvh = blockIdx.x / rows % pg.Hkv, slot = blockIdx.x / rows / pg.Hkv;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, first = WAVES == 4 ? w : 0;
+  const int32_t per = (rows + 4 / WAVES - 1) / (4 / WAVES);                   // workgroups to a tile of a kv head
+  const int32_t kvh = blockIdx.x % pg.Hkv, slot = blockIdx.x / pg.Hkv / per, r = blockIdx.x / pg.Hkv % per * (4 / WAVES) + (WAVES == 4 ? 0 : w);
   TileJob job;
   if (!tile_job<TR>(g, slot, &job) || r >= job.rows) return;
   const int32_t parts = parts_of(g, job.keys);
   if (parts == 1) return;
   const int64_t pr = ((int64_t)slot * pg.Hkv + kvh) * g.splits * TR + r;
-  float best = kNoRef, total = 0.f, y[D / 64];
+  float best = kNoRef, total = 0.f;
+  cols y;
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) y[i] = 0.f;
-  for (int32_t k = w; k < parts; k += 4) {
-    const float pm = g.part_ml[2 * (pr + (int64_t)k * TR)], pl = g.part_ml[2 * (pr + (int64_t)k * TR) + 1];
-    const float next = fmaxf(best, pm), keep = __builtin_amdgcn_exp2f(best - next), f = __builtin_amdgcn_exp2f(pm - next);
+  for (int32_t k0 = first; k0 < parts; k0 += 64 * WAVES) {
+    const int32_t mine = k0 + l * WAVES, n = min((parts - k0 + WAVES - 1) / WAVES, 64);
+    const bool real = mine < parts;
+    const f32x2 st = real ? *(const f32x2*)(g.part_ml + 2 * (pr + (int64_t)mine * TR)) : f32x2{kNoRef, 0.f};
+    float top = st[0];
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+    const float next = fmaxf(best, top), keep = __builtin_amdgcn_exp2f(best - next), f = real ? __builtin_amdgcn_exp2f(st[0] - next) : 0.f;
     best = next;
-    total = total * keep + pl * f;
+    float sum = st[1] * f;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) y[i] = y[i] * keep + g.part_o[(pr + (int64_t)k * TR) * D + l + 64 * i] * f;
-  }
+    for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+    total = total * keep + sum;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) sums[w][l + 64 * i] = y[i];
-  if (l == 0) {
-    stat[w][0] = best;
-    stat[w][1] = total;
-  }
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  best = fmaxf(fmaxf(stat[0][0], stat[1][0]), fmaxf(stat[2][0], stat[3][0]));
-  total = 0.f;
-  float z = 0.f;
+    for (int i = 0; i < D / 64; ++i) y[i] *= keep;
+    const float* at = g.part_o + (pr + (int64_t)k0 * TR) * D + l * (D / 64);
+    for (int32_t k = 0; k < n; k += 8) {         // eight parts on their way at once; what is over is the last one times the 0 of a lane
+      cols v[8];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float f = __builtin_amdgcn_exp2f(stat[k][0] - best);
-    total += stat[k][1] * f;
-    z += sums[k][threadIdx.x] * f;
+      for (int j = 0; j < 8; ++j) v[j] = *(const cols*)(at + (int64_t)min(k + j, n - 1) * WAVES * TR * D);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float fk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + j));
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) y[i] += v[j][i] * fk;
+      }
+    }
   }
-  const int32_t row = job.row0 + r, x = row / pg.group, token = job.first + x, ob = token / a.o.t, ot = token - ob * a.o.t;
-  T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st;
-  out[threadIdx.x] = (T)(total == 0.f ? 0.f : z / total);
+  if constexpr (WAVES == 4) {
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) sums[w][l * (D / 64) + i] = y[i];
+    if (l == 0) {
+      stat[w][0] = best;
+      stat[w][1] = total;
+    }
+    __syncthreads();
+    if (w) return;
+    best = fmaxf(fmaxf(stat[0][0], stat[1][0]), fmaxf(stat[2][0], stat[3][0]));
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) y[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = __builtin_amdgcn_exp2f(stat[k][0] - best);
+      total += stat[k][1] * f;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) y[i] += sums[k][l * (D / 64) + i] * f;
+    }
+  }
+  const int32_t row = job.row0 + r, x = row / pg.group, token = job.first + x, ob = token < a.o.t ? 0 : token / a.o.t, ot = token - ob * a.o.t;
+  T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st + l * (D / 64);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) out[i] = (T)(y[i] * inv);
 }
 
 bool tile_fits(int d) { return d == 64 || d == 128; }
 
 // How the work is dealt out.  Row tiles of 32 where a request has more than 16 rows (new rows times the group) and rows are bf16.
-// Parts of the keys: as many as bring the launch to about kTileTarget workgroups, a part of 256 keys at least (one tile a wave).
-constexpr int kTileTarget = 1024;
+// Parts of the keys, of 256 at least (one tile a wave): as many as bring the launch to the workgroups that are resident at once, two a
+// compute unit: more of them only add their starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless
+// requests differ in length: then those of a batch of single tokens are cut half as long, so that short ones make room (32 requests of
+// 128 .. 8192 keys: 27 us, without 36).
 struct TilePlan { int qb, rows, slots, splits, chunk, by_request; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   TilePlan p{};
@@ -559,7 +595,8 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   const int64_t keys = a.max_held > 0 ? a.max_held : 1;
   constexpr int64_t kLeast = kTileWaves * kTileKeys;
   // not fewer parts for more keys: a workspace for many takes fewer
-  const int64_t want = std::max<int64_t>(kTileTarget / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
+  const int64_t resident = 2 * (int64_t)cu_count(), target = p.by_request && a.n > 1 && units < resident ? 2 * resident : resident;
+  const int64_t want = std::max<int64_t>(target / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
   p.splits = (int)splits;
   p.chunk = (int)std::max<int64_t>(kLeast, ((keys + splits - 1) / splits + kTileKeys - 1) / kTileKeys * kTileKeys);
   p.rows_all = (size_t)p.slots * a.pg.Hkv * p.splits * tr;
@@ -570,8 +607,11 @@ template <typename T, int D, int QB>
 hipError_t launch_tile(const TileArgs& g, const TilePlan& p, hipStream_t s) {
   const unsigned grid = (unsigned)p.slots * (unsigned)p.splits * (unsigned)g.a.pg.Hkv;
   pages_attn_tile_k<T, D, QB><<<grid, 64 * kTileWaves, 0, s>>>(g);
-  if (p.splits > 1)
-    pages_attn_join_k<T, D, 16 * QB><<<(unsigned)p.slots * (unsigned)g.a.pg.Hkv * (unsigned)p.rows, 256, 0, s>>>(g, p.rows);
+  if (p.splits > 1) {
+    const unsigned tiles = (unsigned)p.slots * (unsigned)g.a.pg.Hkv, rows = (unsigned)p.rows;
+    if (p.splits > 16) pages_attn_join_k<T, D, 16 * QB, 4><<<tiles * rows, 256, 0, s>>>(g, p.rows);
+    else pages_attn_join_k<T, D, 16 * QB, 1><<<tiles * ((rows + 3) / 4), 256, 0, s>>>(g, p.rows);
+  }
   return hipGetLastError();
 }
 
