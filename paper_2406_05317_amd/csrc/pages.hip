@@ -9,6 +9,7 @@ namespace {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;      // fp32 rows begin at any float
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Plan.  Three running sums over the requests give every row's place: of the new rows (where a request's rows begin in the call), of
@@ -179,7 +180,11 @@ template <typename T>
 __device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
   if constexpr (std::is_same<T, float>::value) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i];
+    for (int i = 0; i < 2; ++i) {
+      const f32x4_any v = *(const f32x4_any*)(p + 4 * i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
+    }
   } else {
     const u32x4 v = *(const u32x4*)p;
 #pragma unroll
@@ -203,27 +208,30 @@ __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsV
   const int32_t slot = slots[token];
   const int32_t page = slot >> pg.page_shift, row = slot & (pg.page_rows - 1);
   if (slot < 0 || page >= pg.n_pages) return;
-  const bool is_v = blockIdx.z;
-  float x[8];
-  read8(row_of<T>(is_v ? v : k, token, head) + 8 * c, x);
-  uint32_t top = 0;                              // magnitudes as whole numbers: their order, with infinities and NaN on top
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  const int32_t e = (int32_t)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
-  const uint32_t byte = top >= 0x7f800000u ? 255u : (uint32_t)(min(max(e, kMinExp), kMaxExp) + 127);
-  uint32_t code = 0;
-  if (byte != 255u) {
-    const float s = __uint_as_float(byte << 23);
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], s, 0);
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], s, 1);
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], s, 2);
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], s, 3);
-  }
+  float x[2][8];
+  read8(row_of<T>(k, token, head) + 8 * c, x[0]);
+  read8(row_of<T>(v, token, head) + 8 * c, x[1]);
   const int64_t at = (int64_t)page * pg.Hkv + head;
-  *(uint32_t*)((is_v ? pg.v_codes : pg.k_codes) + (at * pg.page_rows + row) * (pg.d / 2) + 4 * c) = code;
-  if ((c & 3) == 0) (is_v ? pg.v_scales : pg.k_scales)[(at * (pg.d / 32) + c / 4) * pg.page_rows + row] = (uint8_t)byte;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    uint32_t top = 0;                            // magnitudes as whole numbers: their order, with infinities and NaN on top
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[j][i]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const int32_t e = (int32_t)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
+    const uint32_t byte = top >= 0x7f800000u ? 255u : (uint32_t)(min(max(e, kMinExp), kMaxExp) + 127);
+    uint32_t code = 0;
+    if (byte != 255u) {
+      const float s = __uint_as_float(byte << 23);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][0], x[j][1], s, 0);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][2], x[j][3], s, 1);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][4], x[j][5], s, 2);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][6], x[j][7], s, 3);
+    }
+    *(uint32_t*)((j ? pg.v_codes : pg.k_codes) + (at * pg.page_rows + row) * (pg.d / 2) + 4 * c) = code;
+    if ((c & 3) == 0) (j ? pg.v_scales : pg.k_scales)[(at * (pg.d / 32) + c / 4) * pg.page_rows + row] = (uint8_t)byte;
+  }
 }
 
 template <typename T>
@@ -232,27 +240,32 @@ __global__ __launch_bounds__(kRowThreads) void pages_load_k(PagesView pg, RowsVi
   if (token >= tokens) return;
   const int32_t slot = slots[token];
   const int32_t page = slot >> pg.page_shift, row = slot & (pg.page_rows - 1);
-  const bool is_v = blockIdx.z;
-  uint32_t code = 0, byte = 127;
+  uint32_t code[2] = {0, 0}, byte[2] = {127, 127};
   if (slot >= 0 && page < pg.n_pages) {
-    const int64_t at = (int64_t)page * pg.Hkv + head;
-    code = *(const uint32_t*)((is_v ? pg.v_codes : pg.k_codes) + (at * pg.page_rows + row) * (pg.d / 2) + 4 * c);
-    byte = (is_v ? pg.v_scales : pg.k_scales)[(at * (pg.d / 32) + c / 4) * pg.page_rows + row];
+    const int64_t at = (int64_t)page * pg.Hkv + head, codes = (at * pg.page_rows + row) * (pg.d / 2) + 4 * c,
+                  scale = (at * (pg.d / 32) + c / 4) * pg.page_rows + row;
+    code[0] = *(const uint32_t*)(pg.k_codes + codes);
+    code[1] = *(const uint32_t*)(pg.v_codes + codes);
+    byte[0] = pg.k_scales[scale];
+    byte[1] = pg.v_scales[scale];
   }
-  const float s = __uint_as_float(byte << 23);
-  T* out = const_cast<T*>(row_of<T>(is_v ? v : k, token, head)) + 8 * c;
-  if constexpr (std::is_same<T, float>::value) {
-    f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 1),
-                  __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 3)};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = y[i / 2][i % 2];
-  } else {
-    u32x4 y;
-    y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0));
-    y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1));
-    y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2));
-    y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3));
-    *(u32x4*)out = y;
+  for (int j = 0; j < 2; ++j) {
+    const float s = __uint_as_float(byte[j] << 23);
+    T* out = const_cast<T*>(row_of<T>(j ? v : k, token, head)) + 8 * c;
+    if constexpr (std::is_same<T, float>::value) {
+      const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 3)};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *(f32x4_any*)(out + 4 * i) = f32x4_any{y[2 * i][0], y[2 * i][1], y[2 * i + 1][0], y[2 * i + 1][1]};
+    } else {
+      u32x4 y;
+      y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 0));
+      y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 1));
+      y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 2));
+      y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 3));
+      *(u32x4*)out = y;
+    }
   }
 }
 
@@ -260,7 +273,7 @@ __global__ __launch_bounds__(kRowThreads) void pages_load_k(PagesView pg, RowsVi
 dim3 row_block(const PagesView& pg) { return dim3((unsigned)(pg.d / 8), (unsigned)(kRowThreads / (pg.d / 8))); }
 dim3 row_grid(const PagesView& pg, int32_t tokens) {
   const int rows = kRowThreads / (pg.d / 8);
-  return dim3((unsigned)((tokens + rows - 1) / rows), (unsigned)pg.Hkv, 2);
+  return dim3((unsigned)((tokens + rows - 1) / rows), (unsigned)pg.Hkv);
 }
 
 }  // namespace

@@ -129,11 +129,14 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 //     the D/32 bytes of columns D/16 m .. + D/16 - 1 and pairs two keys' values of a column after the conversion.
 //
 // Running softmax: the reference a row's exponentials are taken against moves only when a tile's largest score passes it by 8 (in powers
-// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits; one alone is off
-// by as much as the rounding of a bf16 result, where few keys carry a row by more than a test of that rounding allows), for fp32 rows of
-// three (all 24 bits), as their queries do.  Their sum is taken of the same numbers, by a product with ones: no vector instruction adds.
+// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits) in every tile where
+// one of them is more than an eighth of what its row has summed up so far, as one in the others: their roundings, of either sign and each
+// at most 2^-8 of an eighth, then leave the result some 2^-11 off, below the rounding of a bf16 result (where few keys carry a row, one
+// part alone would double that).  For fp32 rows three numbers (all 24 bits), as their queries do.  Their sum is taken of the same
+// numbers, by a product with ones: no vector instruction adds.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
+constexpr float kFine = 0.125f;                // a probability above this share of its row's sum so far takes its second part along
 
 typedef __attribute__((ext_vector_type(4))) float f4;
 
@@ -232,25 +235,31 @@ __device__ __forceinline__ float max_groups(float x) {
   return max_halves(x);
 }
 
-// the page of a key as a lane needs it: -1 where there is none
-__device__ __forceinline__ int32_t page_of(const PagesAttnArgs& a, const int32_t* table, int32_t key, int32_t held) {
-  const int32_t page = key < held ? table[key >> a.pg.page_shift] : -1;
-  return (uint32_t)page < (uint32_t)a.pg.n_pages ? page : -1;
+// the page of a key: -1 where there is none, and behind the keys at hand (without a branch: an entry is read in any case)
+__device__ __forceinline__ int32_t page_of(const PagesAttnArgs& a, const int32_t* table, int32_t key, int32_t keys) {
+  const int32_t page = table[max(min(key, keys - 1), 0) >> a.pg.page_shift];
+  const bool in = (key < keys) & ((uint32_t)page < (uint32_t)a.pg.n_pages);
+  return in ? page : -1;
 }
 
+// (rows of a page are always there; a lane without a page reads page 0 and has its keys masked)
 template <int D>
-__device__ __forceinline__ void load_tile(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t kpage, int32_t vpage, int m,
-                                          int g) {
-  const int32_t krow = (key0 + 4 * m) & (pg.page_rows - 1), vrow = (key0 + 16 * g) & (pg.page_rows - 1);
-  const int64_t kat = ((int64_t)max(kpage, 0) * pg.Hkv + kvh) * pg.page_rows, vat = ((int64_t)max(vpage, 0) * pg.Hkv + kvh) * pg.page_rows;
-  const uint8_t* kc = pg.k_codes + (kat + krow) * (D / 2) + g * (D / 8);
-  const uint8_t* vc = pg.v_codes + (vat + vrow) * (D / 2) + m * (D / 32);
+__device__ __forceinline__ void load_k(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
+  const int32_t row = (key0 + 4 * m) & (pg.page_rows - 1);
+  const int64_t at = ((int64_t)max(page, 0) * pg.Hkv + kvh) * pg.page_rows;
+  const uint8_t* codes = pg.k_codes + (at + row) * (D / 2) + g * (D / 8);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) c.k[t] = *(const typename Bytes<D / 8>::type*)(kc + t * (D / 2));
-  c.ks = *(const uint32_t*)(pg.k_scales + kat * (D / 32) + (g * (D / 4) / 32) * pg.page_rows + krow);
+  for (int t = 0; t < 4; ++t) c.k[t] = *(const typename Bytes<D / 8>::type*)(codes + t * (D / 2));
+  c.ks = *(const uint32_t*)(pg.k_scales + at * (D / 32) + (g * (D / 4) / 32) * pg.page_rows + row);
+}
+template <int D>
+__device__ __forceinline__ void load_v(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
+  const int32_t row = (key0 + 16 * g) & (pg.page_rows - 1);
+  const int64_t at = ((int64_t)max(page, 0) * pg.Hkv + kvh) * pg.page_rows;
+  const uint8_t* codes = pg.v_codes + (at + row) * (D / 2) + m * (D / 32);
 #pragma unroll
-  for (int x = 0; x < 16; ++x) c.v[x] = *(const typename Bytes<D / 32>::type*)(vc + x * (D / 2));
-  c.vs = *(const u32x4*)(pg.v_scales + vat * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + vrow);
+  for (int x = 0; x < 16; ++x) c.v[x] = *(const typename Bytes<D / 32>::type*)(codes + x * (D / 2));
+  c.vs = *(const u32x4*)(pg.v_scales + at * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + row);
 }
 
 template <typename T, int D, int QB>
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   __shared__ int32_t nan_key[D / 32];          // first visible key whose 32 values of V stand for NaN, among the tiles that mask
   const PagesAttnArgs& a = g.a;
   const PagesView& pg = a.pg;
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, m = l & 15, grp = l >> 4;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = l & 15, grp = l >> 4;
   const int item = xcd_item(blockIdx.x, gridDim.x);
   // neighbours, on one XCD: the kv heads of a part where a request is one tile (their scales share cache lines), else the tiles that
   // read the same keys
@@ -323,13 +332,19 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   int32_t key0 = key_lo + w * kTileKeys;
   int32_t kp = page_of(a, table, key0 + 4 * m, key_hi), vp = page_of(a, table, key0 + 16 * grp, key_hi);
   TileCodes<D> cur;
-  if (key0 < key_hi) load_tile<D>(cur, pg, kvh, key0, kp, vp, m, grp);
+  if (key0 < key_hi) {
+    load_k<D>(cur, pg, kvh, key0, kp, m, grp);
+    load_v<D>(cur, pg, kvh, key0, vp, m, grp);
+  }
   int32_t kp1 = page_of(a, table, key0 + kStride + 4 * m, key_hi), vp1 = page_of(a, table, key0 + kStride + 16 * grp, key_hi);
   while (key0 < key_hi) {
     TileCodes<D> nxt;
     const int32_t key1 = key0 + kStride;
     const bool more = key1 < key_hi;
-    if (more) load_tile<D>(nxt, pg, kvh, key1, kp1, vp1, m, grp);
+    if (more) {
+      load_k<D>(nxt, pg, kvh, key1, kp1, m, grp);
+      load_v<D>(nxt, pg, kvh, key1, vp1, m, grp);
+    }
     const int32_t kp2 = page_of(a, table, key1 + kStride + 4 * m, key_hi), vp2 = page_of(a, table, key1 + kStride + 16 * grp, key_hi);
 
     f4 s[QB][4];
@@ -367,7 +382,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         if (!in || odd) vs[x / 4] &= ~(255u << (8 * (x % 4)));
       }
     }
-    bf16x8 p[QB][PROBS][2];
+    bool fine = PROBS == 3;                      // whether the tile's probabilities need more than their first part
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float top = s[qb][0][0];
@@ -383,6 +398,11 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
 #pragma unroll
         for (int j = 0; j < COLS; ++j) o[qb][j] = f4{o[qb][j][0] * keep, o[qb][j][1] * keep, o[qb][j][2] * keep, o[qb][j][3] * keep};
       }
+      if constexpr (PROBS == 2) fine |= __any(__builtin_amdgcn_exp2f(top - ref[qb]) > kFine * sum[qb][0]);
+    }
+    bf16x8 p[QB][PROBS][2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float e[8];                             // keys 16 grp + 8 h + 4 i + t
@@ -391,14 +411,19 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
 #pragma unroll
           for (int t = 0; t < 4; ++t) e[4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
         bf16x8 part[PROBS];
-        split_parts<PROBS>(e, part);
+        if (fine) {
+          split_parts<PROBS>(e, part);
 #pragma unroll
-        for (int k = PROBS - 1; k >= 0; --k) {
-          p[qb][k][h] = part[k];
-          sum[qb] = mfma16(ones, part[k], sum[qb]);
+          for (int k = PROBS - 1; k > 0; --k) sum[qb] = mfma16(ones, part[k], sum[qb]);
+        } else {
+          bf16x8 one[1];
+          split_parts<1>(e, one);
+          part[0] = one[0];
         }
+        sum[qb] = mfma16(ones, part[0], sum[qb]);
+#pragma unroll
+        for (int k = 0; k < PROBS; ++k) p[qb][k][h] = part[k];
       }
-    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float sc[8];
@@ -416,12 +441,19 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
           odd[x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x07060302u);
         }
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
+        for (int qb = 0; qb < QB; ++qb) {
+          o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][0][h], o[qb][2 * B]);
+          o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][0][h], o[qb][2 * B + 1]);
+        }
+        if (fine) {
 #pragma unroll
-          for (int k = PROBS - 1; k >= 0; --k) {
-            o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][k][h], o[qb][2 * B]);
-            o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][k][h], o[qb][2 * B + 1]);
-          }
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int k = 1; k < PROBS; ++k) {
+              o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][k][h], o[qb][2 * B]);
+              o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][k][h], o[qb][2 * B + 1]);
+            }
+        }
       };
       columns(std::integral_constant<int, 0>());
       columns(std::integral_constant<int, 1>());
@@ -581,12 +613,12 @@ bool tile_fits(int d) { return d == 64 || d == 128; }
 // compute unit: more of them only add their starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless
 // requests differ in length: then those of a batch of single tokens are cut half as long, so that short ones make room (32 requests of
 // 128 .. 8192 keys: 27 us, without 36).
-struct TilePlan { int qb, rows, slots, splits, chunk, by_request; size_t rows_all; };
+struct TilePlan { int tr, rows, slots, splits, chunk, by_request; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   TilePlan p{};
   const int64_t most = (int64_t)a.max_new * a.pg.group;
-  p.qb = dtype == LOCOCO_BF16 && most > 16 ? 2 : 1;
-  const int tr = 16 * p.qb;
+  p.tr = dtype != LOCOCO_BF16 || most <= 16 ? 16 : 32;
+  const int tr = p.tr;
   p.by_request = most <= tr;
   p.rows = (int)(most < tr ? most : tr);
   p.slots = p.by_request ? a.n : (int)((int64_t)a.tokens * a.pg.group / tr) + a.n;
@@ -603,16 +635,22 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   return p;
 }
 
-template <typename T, int D, int QB>
+template <typename T, int D, int TR>
 hipError_t launch_tile(const TileArgs& g, const TilePlan& p, hipStream_t s) {
-  const unsigned grid = (unsigned)p.slots * (unsigned)p.splits * (unsigned)g.a.pg.Hkv;
-  pages_attn_tile_k<T, D, QB><<<grid, 64 * kTileWaves, 0, s>>>(g);
+  const unsigned tiles = (unsigned)p.slots * (unsigned)g.a.pg.Hkv, grid = tiles * (unsigned)p.splits, rows = (unsigned)p.rows;
+  pages_attn_tile_k<T, D, TR / 16><<<grid, 64 * kTileWaves, 0, s>>>(g);
   if (p.splits > 1) {
-    const unsigned tiles = (unsigned)p.slots * (unsigned)g.a.pg.Hkv, rows = (unsigned)p.rows;
-    if (p.splits > 16) pages_attn_join_k<T, D, 16 * QB, 4><<<tiles * rows, 256, 0, s>>>(g, p.rows);
-    else pages_attn_join_k<T, D, 16 * QB, 1><<<tiles * ((rows + 3) / 4), 256, 0, s>>>(g, p.rows);
+    if (p.splits > 16) pages_attn_join_k<T, D, TR, 4><<<tiles * rows, 256, 0, s>>>(g, p.rows);
+    else pages_attn_join_k<T, D, TR, 1><<<tiles * ((rows + 3) / 4), 256, 0, s>>>(g, p.rows);
   }
   return hipGetLastError();
+}
+template <typename T, int D>
+hipError_t launch_tiles(const TileArgs& g, const TilePlan& p, hipStream_t s) {
+  if constexpr (!std::is_same<T, float>::value) {
+    if (p.tr == 32) return launch_tile<T, D, 32>(g, p, s);
+  }
+  return launch_tile<T, D, 16>(g, p, s);
 }
 
 }  // namespace
@@ -627,9 +665,8 @@ hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace,
   if (tile_fits(a.pg.d)) {
     const TilePlan p = tile_plan(dtype, a);
     TileArgs g{a, p.splits, p.chunk, p.slots, p.by_request, (float*)workspace, (float*)workspace + p.rows_all * a.pg.d};
-    if (dtype == LOCOCO_F32) return a.pg.d == 64 ? launch_tile<float, 64, 1>(g, p, s) : launch_tile<float, 128, 1>(g, p, s);
-    if (p.qb == 1) return a.pg.d == 64 ? launch_tile<__bf16, 64, 1>(g, p, s) : launch_tile<__bf16, 128, 1>(g, p, s);
-    return a.pg.d == 64 ? launch_tile<__bf16, 64, 2>(g, p, s) : launch_tile<__bf16, 128, 2>(g, p, s);
+    if (dtype == LOCOCO_F32) return a.pg.d == 64 ? launch_tiles<float, 64>(g, p, s) : launch_tiles<float, 128>(g, p, s);
+    return a.pg.d == 64 ? launch_tiles<__bf16, 64>(g, p, s) : launch_tiles<__bf16, 128>(g, p, s);
   }
   const dim3 grid((unsigned)((a.tokens + kRowsWaves - 1) / kRowsWaves), (unsigned)a.pg.Hq);
   if (dtype == LOCOCO_F32) pages_attn_rows_k<float><<<grid, 64 * kRowsWaves, 0, s>>>(a);
