@@ -160,13 +160,18 @@ __device__ __forceinline__ bool tile_job(const TileArgs& g, int32_t slot, TileJo
   const PagesAttnArgs& a = g.a;
   int32_t req = slot, tile = 0;
   if (!g.by_request) {
-    // request i's tiles begin at slot starts[i] * group / TR + i: with that a request's tiles never reach into the next one's
-    int lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((int32_t)((int64_t)a.starts[mid] * a.pg.group / TR) + mid <= slot) lo = mid; else hi = mid;
+    // request i's tiles begin at slot starts[i] * group / TR + i: with that a request's tiles never reach into the next one's.  The last
+    // request that begins at or before the slot, 64 candidates at a look (one trip to memory, two with more than 64 requests).
+    const int l = threadIdx.x & 63;
+    req = 0;
+#pragma unroll
+    for (int step = 64; step; step = step == 64 ? 1 : 0) {
+      if (step == 64 && a.n <= 64) continue;
+      const int i = min(req + l * step, a.n - 1);
+      const int32_t at = (int32_t)((int64_t)a.starts[i] * a.pg.group / TR) + i;
+      req += max(__popcll(__ballot(req + l * step < a.n && at <= slot)) - 1, 0) * step;
     }
-    req = lo;
+    req = __builtin_amdgcn_readfirstlane(req);
     tile = slot - (int32_t)((int64_t)a.starts[req] * a.pg.group / TR) - req;
     if (tile < 0) return false;
   }
@@ -203,17 +208,20 @@ struct Bytes<2> { typedef uint16_t type; };
 
 // the codes and scales of a tile, as a lane holds them
 template <int D>
-struct TileCodes {
-  typename Bytes<D / 8>::type k[4];            // keys 4 m + t
-  uint32_t ks;                                 // their scales, a byte each
-  typename Bytes<D / 32>::type v[16];          // keys 16 g + x
-  u32x4 vs;
+struct KeyCodes {
+  typename Bytes<D / 8>::type c[4];            // keys 4 m + t
+  uint32_t scales;                             // a byte each
+};
+template <int D>
+struct ValueCodes {
+  typename Bytes<D / 32>::type c[16];          // keys 16 g + x
+  u32x4 scales;
 };
 
 // key t's bf16 operand of a step: 8 values
 template <int D>
-__device__ __forceinline__ bf16x8 k_operand(const TileCodes<D>& c, int t, int step, float scale) {
-  const uint32_t w = c.k[t][step];
+__device__ __forceinline__ bf16x8 k_operand(const KeyCodes<D>& k, int t, int step, float scale) {
+  const uint32_t w = k.c[t][step];
   u32x4 r;
   r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
   r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
@@ -244,22 +252,22 @@ __device__ __forceinline__ int32_t page_of(const PagesAttnArgs& a, const int32_t
 
 // (rows of a page are always there; a lane without a page reads page 0 and has its keys masked)
 template <int D>
-__device__ __forceinline__ void load_k(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
+__device__ __forceinline__ void load_k(KeyCodes<D>& k, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
   const int32_t row = (key0 + 4 * m) & (pg.page_rows - 1);
   const int64_t at = ((int64_t)max(page, 0) * pg.Hkv + kvh) * pg.page_rows;
   const uint8_t* codes = pg.k_codes + (at + row) * (D / 2) + g * (D / 8);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) c.k[t] = *(const typename Bytes<D / 8>::type*)(codes + t * (D / 2));
-  c.ks = *(const uint32_t*)(pg.k_scales + at * (D / 32) + (g * (D / 4) / 32) * pg.page_rows + row);
+  for (int t = 0; t < 4; ++t) k.c[t] = *(const typename Bytes<D / 8>::type*)(codes + t * (D / 2));
+  k.scales = *(const uint32_t*)(pg.k_scales + at * (D / 32) + (g * (D / 4) / 32) * pg.page_rows + row);
 }
 template <int D>
-__device__ __forceinline__ void load_v(TileCodes<D>& c, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
+__device__ __forceinline__ void load_v(ValueCodes<D>& v, const PagesView& pg, int32_t kvh, int32_t key0, int32_t page, int m, int g) {
   const int32_t row = (key0 + 16 * g) & (pg.page_rows - 1);
   const int64_t at = ((int64_t)max(page, 0) * pg.Hkv + kvh) * pg.page_rows;
   const uint8_t* codes = pg.v_codes + (at + row) * (D / 2) + m * (D / 32);
 #pragma unroll
-  for (int x = 0; x < 16; ++x) c.v[x] = *(const typename Bytes<D / 32>::type*)(codes + x * (D / 2));
-  c.vs = *(const u32x4*)(pg.v_scales + at * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + row);
+  for (int x = 0; x < 16; ++x) v.c[x] = *(const typename Bytes<D / 32>::type*)(codes + x * (D / 2));
+  v.scales = *(const u32x4*)(pg.v_scales + at * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + row);
 }
 
 template <typename T, int D, int QB>
@@ -329,40 +337,30 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   }
 
   constexpr int kStride = kTileWaves * kTileKeys;
-  int32_t key0 = key_lo + w * kTileKeys;
-  int32_t kp = page_of(a, table, key0 + 4 * m, key_hi), vp = page_of(a, table, key0 + 16 * grp, key_hi);
-  TileCodes<D> cur;
-  if (key0 < key_hi) {
-    load_k<D>(cur, pg, kvh, key0, kp, m, grp);
-    load_v<D>(cur, pg, kvh, key0, vp, m, grp);
-  }
-  int32_t kp1 = page_of(a, table, key0 + kStride + 4 * m, key_hi), vp1 = page_of(a, table, key0 + kStride + 16 * grp, key_hi);
-  while (key0 < key_hi) {
-    TileCodes<D> nxt;
-    const int32_t key1 = key0 + kStride;
-    const bool more = key1 < key_hi;
-    if (more) {
-      load_k<D>(nxt, pg, kvh, key1, kp1, m, grp);
-      load_v<D>(nxt, pg, kvh, key1, vp1, m, grp);
-    }
-    const int32_t kp2 = page_of(a, table, key1 + kStride + 4 * m, key_hi), vp2 = page_of(a, table, key1 + kStride + 16 * grp, key_hi);
-
+  int32_t key0 = key_lo + w * kTileKeys, kp = page_of(a, table, key0 + 4 * m, key_hi);
+  KeyCodes<D> kc;
+  if (key0 < key_hi) load_k<D>(kc, pg, kvh, key0, kp, m, grp);
+  kp = page_of(a, table, key0 + kStride + 4 * m, key_hi);
+  // one tile: vp is the page of a lane's keys
+  auto tile = [&](const ValueCodes<D>& vc, int32_t vp) {
     f4 s[QB][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float sc = scale_byte(cur.ks, t);
+      const float sc = scale_byte(kc.scales, t);
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) s[qb][t] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
-        const bf16x8 k = k_operand<D>(cur, t, st, sc);
+        const bf16x8 k = k_operand<D>(kc, t, st, sc);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) s[qb][t] = mfma16(k, q[qb][p][st], s[qb][t]);
       }
     }
-    u32x4 vs = cur.vs;
+    if (key0 + kStride < key_hi) load_k<D>(kc, pg, kvh, key0 + kStride, kp, m, grp);     // the next tile's, into the same registers
+    kp = page_of(a, table, key0 + 2 * kStride + 4 * m, key_hi);
+    u32x4 vs = vc.scales;
     if (key0 + kTileKeys > min(whole, key_hi) || __any(vp < 0)) {
       // keys behind a row's own, behind the part, or without a page: no score, and a V that is zero times something finite.  A key that
       // only some rows see may stand for NaN: taken out of the product here and put into those rows at the end.
@@ -382,48 +380,65 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         if (!in || odd) vs[x / 4] &= ~(255u << (8 * (x % 4)));
       }
     }
-    bool fine = PROBS == 3;                      // whether the tile's probabilities need more than their first part
+    float top[QB];
+    bool grown = false, carries = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      float top = s[qb][0][0];
+      top[qb] = s[qb][0][0];
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[qb][t][i]);
-      top *= c;
-      if (__any(top > ref[qb] + 8.f)) {
-        const float next = fmaxf(ref[qb], max_groups(top)), keep = __builtin_amdgcn_exp2f(ref[qb] - next);
+        for (int i = 0; i < 4; ++i) top[qb] = fmaxf(top[qb], s[qb][t][i]);
+      top[qb] *= c;
+      grown |= top[qb] > ref[qb] + 8.f;
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const float next = fmaxf(ref[qb], max_groups(top[qb])), keep = __builtin_amdgcn_exp2f(ref[qb] - next);
         ref[qb] = next;
         sum[qb] = f4{sum[qb][0] * keep, sum[qb][1] * keep, sum[qb][2] * keep, sum[qb][3] * keep};
 #pragma unroll
         for (int j = 0; j < COLS; ++j) o[qb][j] = f4{o[qb][j][0] * keep, o[qb][j][1] * keep, o[qb][j][2] * keep, o[qb][j][3] * keep};
       }
-      if constexpr (PROBS == 2) fine |= __any(__builtin_amdgcn_exp2f(top - ref[qb]) > kFine * sum[qb][0]);
     }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) carries |= __builtin_amdgcn_exp2f(top[qb] - ref[qb]) > kFine * sum[qb][0];
+    const bool fine = PROBS == 3 || __any(carries);      // whether the tile's probabilities need more than their first part
+
     bf16x8 p[QB][PROBS][2];
+    float e[QB][2][8];                          // keys 16 grp + 8 h + 4 i + t; then what their first part leaves
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float e[8];                             // keys 16 grp + 8 h + 4 i + t
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) e[4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
-        bf16x8 part[PROBS];
-        if (fine) {
-          split_parts<PROBS>(e, part);
-#pragma unroll
-          for (int k = PROBS - 1; k > 0; --k) sum[qb] = mfma16(ones, part[k], sum[qb]);
-        } else {
-          bf16x8 one[1];
-          split_parts<1>(e, one);
-          part[0] = one[0];
-        }
-        sum[qb] = mfma16(ones, part[0], sum[qb]);
-#pragma unroll
-        for (int k = 0; k < PROBS; ++k) p[qb][k][h] = part[k];
+          for (int t = 0; t < 4; ++t) e[qb][h][4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
+        bf16x8 part[1];
+        split_parts<1>(e[qb][h], part);
+        p[qb][0][h] = part[0];
       }
+    if (fine) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 part[PROBS];
+          split_parts<PROBS>(e[qb][h], part);
+#pragma unroll
+          for (int k = PROBS - 1; k > 0; --k) {
+            p[qb][k][h] = part[k];
+            sum[qb] = mfma16(ones, part[k], sum[qb]);
+          }
+        }
+    }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sum[qb] = mfma16(ones, p[qb][0][h], sum[qb]);
+
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float sc[8];
@@ -433,26 +448,23 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         constexpr int B = decltype(byte)::value;
         uint32_t y[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) y[x] = v_pair<B>(cur.v[8 * h + x], sc[x]);
-        u32x4 even, odd;
+        for (int x = 0; x < 8; ++x) y[x] = v_pair<B>(vc.c[8 * h + x], sc[x]);
+        u32x4 op[2];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          even[x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x05040100u);
-          odd[x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x07060302u);
+          op[0][x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x05040100u);
+          op[1][x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x07060302u);
         }
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][0][h], o[qb][2 * B]);
-          o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][0][h], o[qb][2 * B + 1]);
-        }
-        if (fine) {
+        auto products = [&](int k) {
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-            for (int k = 1; k < PROBS; ++k) {
-              o[qb][2 * B] = mfma16(__builtin_bit_cast(bf16x8, even), p[qb][k][h], o[qb][2 * B]);
-              o[qb][2 * B + 1] = mfma16(__builtin_bit_cast(bf16x8, odd), p[qb][k][h], o[qb][2 * B + 1]);
-            }
+            for (int j = 0; j < 2; ++j) o[qb][2 * B + j] = mfma16(__builtin_bit_cast(bf16x8, op[j]), p[qb][k][h], o[qb][2 * B + j]);
+        };
+        products(0);
+        if (fine) {
+#pragma unroll
+          for (int k = 1; k < PROBS; ++k) products(k);
         }
       };
       columns(std::integral_constant<int, 0>());
@@ -462,12 +474,25 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         columns(std::integral_constant<int, 3>());
       }
     }
-    cur = nxt;
-    key0 = key1;
-    kp = kp1;
-    vp = vp1;
-    kp1 = kp2;
-    vp1 = vp2;
+    key0 += kStride;
+  };
+  // two tiles a turn: the codes of V are on their way a whole tile ahead, each tile's in registers of its own
+  if (key0 < key_hi) {
+    ValueCodes<D> even, odd;
+    int32_t vp = page_of(a, table, key0 + 16 * grp, key_hi), vp1 = page_of(a, table, key0 + kStride + 16 * grp, key_hi);
+    load_v<D>(even, pg, kvh, key0, vp, m, grp);
+    while (true) {
+      int32_t vp2 = page_of(a, table, key0 + 2 * kStride + 16 * grp, key_hi);
+      if (key0 + kStride < key_hi) load_v<D>(odd, pg, kvh, key0 + kStride, vp1, m, grp);
+      tile(even, vp);
+      if (key0 >= key_hi) break;
+      vp = vp2;
+      vp2 = page_of(a, table, key0 + 2 * kStride + 16 * grp, key_hi);
+      if (key0 + kStride < key_hi) load_v<D>(even, pg, kvh, key0 + kStride, vp, m, grp);
+      tile(odd, vp1);
+      if (key0 >= key_hi) break;
+      vp1 = vp2;
+    }
   }
 
   // the four waves' results to one: o[qb][j][i] is column COLS (4 grp + i) + j of row 16 qb + m

@@ -411,3 +411,14 @@ def test_refusals():
     many = torch.zeros(5000, **I32)
     assert status(lb.lococo_pages_plan, pages, many, many.clone(), torch.zeros(5000, 3, **I32), ring, ends, many.clone(), e2,
                   torch.zeros(5001, **I32), slots, pos, totals) == lb.LOCOCO_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("n", [64, 65, 130, 700])
+@pytest.mark.parametrize("group", [1, 20])
+def test_attention_of_many_requests(n, group):
+    """Requests of none to many rows side by side, more of them than one look at their starts takes in."""
+    r = random.Random(n)
+    lens = [(r.randint(0, 40), r.choice([0, 1, 1, 2, 3])) for _ in range(n)]
+    lens[n // 2], lens[-1] = (90, 75 if group == 1 else 5), (33, 4)
+    batch = make_batch(81, torch.bfloat16, 1, group, 64, 16, lens)
+    check_attn(*batch, run_attn(*batch))
