@@ -634,10 +634,13 @@ __global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t row
 bool tile_fits(int d) { return d == 64 || d == 128; }
 
 // How the work is dealt out.  Row tiles of 32 where a request has more than 16 rows (new rows times the group) and rows are bf16.
-// Parts of the keys, of 256 at least (one tile a wave): as many as bring the launch to the workgroups that are resident at once, two a
-// compute unit: more of them only add their starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless
-// requests differ in length: then those of a batch of single tokens are cut half as long, so that short ones make room (32 requests of
-// 128 .. 8192 keys: 27 us, without 36).
+// Parts of the keys, of 256 at least (one tile a wave):
+//  - none where the longest request is short.  One part takes about 5 us and 1.15 us for 256 keys more, 1.7 where all compute units are
+//    busy; joining parts takes 4.  One request, 8 kv heads: 512 keys 7.6 us whole and 9.2 in parts, 1024 keys 10.2 and 9.3; 32 requests:
+//    1024 keys 13 and 18 us, 2048 keys 18 and 25.
+//  - else as many as bring the launch to the workgroups that are resident at once, two a compute unit: more of them only add their
+//    starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless requests differ in length: those of a
+//    batch of single tokens are cut half as long, so that short ones make room (32 requests of 128 .. 8192 keys: 27 us, without 36).
 struct TilePlan { int tr, rows, slots, splits, chunk, by_request; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   TilePlan p{};
@@ -653,7 +656,8 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   constexpr int64_t kLeast = kTileWaves * kTileKeys;
   // not fewer parts for more keys: a workspace for many takes fewer
   const int64_t resident = 2 * (int64_t)cu_count(), target = p.by_request && a.n > 1 && units < resident ? 2 * resident : resident;
-  const int64_t want = std::max<int64_t>(target / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
+  const int64_t whole = 2 * units >= resident ? 2048 : 768;
+  const int64_t want = keys <= whole ? 1 : std::max<int64_t>(target / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
   p.splits = (int)splits;
   p.chunk = (int)std::max<int64_t>(kLeast, ((keys + splits - 1) / splits + kTileKeys - 1) / kTileKeys * kTileKeys);
   p.rows_all = (size_t)p.slots * a.pg.Hkv * p.splits * tr;
