@@ -500,7 +500,7 @@ def workspace(cfg, L: int, B: int, history: bool = False, device="cuda") -> torc
 
 
 def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int) -> torch.Tensor | None:
-    """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes or smaller batches of them."""
+    """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes (max_held may be larger than theirs)."""
     need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
     return torch.empty(need, dtype=torch.uint8, device=pages.device) if need else None
 

@@ -1796,22 +1796,6 @@ RowsView rows_view(const lococo_tensor* t, int32_t rows_per_batch) {
   return RowsView{t->p, t->stride_b, t->stride_h, t->stride_t, rows_per_batch};
 }
 
-lococo_status check_requests(const lococo_pages* p, const lococo_requests* r, bool arrays) {
-  if (!r) return fail(LOCOCO_EINVAL, "requests is NULL");
-  if (r->n <= 0 || r->tokens < 0 || r->table_pages <= 0 || r->max_new < 0 || r->max_held < 0)
-    return fail(LOCOCO_EINVAL, "n and table_pages must be positive, tokens, max_new and max_held not negative");
-  if (r->n > kPagesMaxRequests) return fail(LOCOCO_EUNSUPPORTED, "more than %d requests", kPagesMaxRequests);
-  if (r->tokens >= kPagesCap || (int64_t)r->table_pages * p->page_rows >= kPagesCap)
-    return fail(LOCOCO_EUNSUPPORTED, "tokens and table_pages * page_rows must be below 2^30 - 1");
-  if ((int64_t)r->max_new * r->n < r->tokens) return fail(LOCOCO_EINVAL, "max_new * n is below tokens");
-  if (arrays) {
-    if (!r->tables || !r->starts || !r->held) return fail(LOCOCO_EINVAL, "an array of the requests is NULL");
-    if (((uintptr_t)r->tables | (uintptr_t)r->starts | (uintptr_t)r->held) & 3)
-      return fail(LOCOCO_EINVAL, "arrays of the requests must be 4-byte aligned");
-  }
-  return LOCOCO_OK;
-}
-
 PagesAttnArgs pages_attn_args(const lococo_pages* p, const lococo_requests* r) {
   PagesAttnArgs a{};
   a.pg = pages_view(p);
@@ -1824,6 +1808,23 @@ PagesAttnArgs pages_attn_args(const lococo_pages* p, const lococo_requests* r) {
   a.starts = r->starts;
   a.held = r->held;
   return a;
+}
+
+lococo_status check_requests(const lococo_pages* p, const lococo_requests* r, bool arrays) {
+  if (!r) return fail(LOCOCO_EINVAL, "requests is NULL");
+  if (r->n <= 0 || r->tokens < 0 || r->table_pages <= 0 || r->max_new < 0 || r->max_held < 0)
+    return fail(LOCOCO_EINVAL, "n and table_pages must be positive, tokens, max_new and max_held not negative");
+  if (r->n > kPagesMaxRequests) return fail(LOCOCO_EUNSUPPORTED, "more than %d requests", kPagesMaxRequests);
+  if (r->tokens >= kPagesCap || (int64_t)r->table_pages * p->page_rows >= kPagesCap)
+    return fail(LOCOCO_EUNSUPPORTED, "tokens and table_pages * page_rows must be below 2^30 - 1");
+  if ((int64_t)r->max_new * r->n < r->tokens) return fail(LOCOCO_EINVAL, "max_new * n is below tokens");
+  if (!pages_attn_fits(p->dtype, pages_attn_args(p, r))) return fail(LOCOCO_EUNSUPPORTED, "more query rows than one launch takes");
+  if (arrays) {
+    if (!r->tables || !r->starts || !r->held) return fail(LOCOCO_EINVAL, "an array of the requests is NULL");
+    if (((uintptr_t)r->tables | (uintptr_t)r->starts | (uintptr_t)r->held) & 3)
+      return fail(LOCOCO_EINVAL, "arrays of the requests must be 4-byte aligned");
+  }
+  return LOCOCO_OK;
 }
 
 }  // namespace

@@ -129,14 +129,13 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 //     the D/32 bytes of columns D/16 m .. + D/16 - 1 and pairs two keys' values of a column after the conversion.
 //
 // Running softmax: the reference a row's exponentials are taken against moves only when a tile's largest score passes it by 8 (in powers
-// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits) in every tile where
-// one of them is more than an eighth of what its row has summed up so far, as one in the others: their roundings, of either sign and each
-// at most 2^-8 of an eighth, then leave the result some 2^-11 off, below the rounding of a bf16 result (where few keys carry a row, one
-// part alone would double that).  For fp32 rows three numbers (all 24 bits), as their queries do.  Their sum is taken of the same
-// numbers, by a product with ones: no vector instruction adds.
+// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits), for fp32
+// rows of three (all 24 bits), as their queries do.  One alone would save a third of the MFMAs (prompts of 2000 tokens 0.81 ms for 0.99),
+// but is off by as much as the rounding of a bf16 result wherever one key carries a column, be it by its probability or, as where new
+// rows stand beside the averages of a compressed memory, by the size of its value.  Their sum is taken of the same numbers, by a product
+// with ones: no vector instruction adds.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
-constexpr float kFine = 0.125f;                // a probability above this share of its row's sum so far takes its second part along
 
 typedef __attribute__((ext_vector_type(4))) float f4;
 
@@ -325,9 +324,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   const int32_t* table = a.tables + (int64_t)job.req * a.table_pages;
   float ref[QB];
   f4 o[QB][COLS], sum[QB];                     // sum: the same number in all four places of a lane
-  bf16x8 ones;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+  constexpr int kStride = kTileWaves * kTileKeys;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     ref[qb] = kNoRef;
@@ -335,9 +332,8 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
 #pragma unroll
     for (int j = 0; j < COLS; ++j) o[qb][j] = f4{0.f, 0.f, 0.f, 0.f};
   }
-
-  constexpr int kStride = kTileWaves * kTileKeys;
-  int32_t key0 = key_lo + w * kTileKeys, kp = page_of(a, table, key0 + 4 * m, key_hi);
+  int32_t key0 = key_lo + w * kTileKeys;
+  int32_t kp = page_of(a, table, key0 + 4 * m, key_hi);
   KeyCodes<D> kc;
   if (key0 < key_hi) load_k<D>(kc, pg, kvh, key0, kp, m, grp);
   kp = page_of(a, table, key0 + kStride + 4 * m, key_hi);
@@ -381,7 +377,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
       }
     }
     float top[QB];
-    bool grown = false, carries = false;
+    bool grown = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       top[qb] = s[qb][0][0];
@@ -402,42 +398,25 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         for (int j = 0; j < COLS; ++j) o[qb][j] = f4{o[qb][j][0] * keep, o[qb][j][1] * keep, o[qb][j][2] * keep, o[qb][j][3] * keep};
       }
     }
+    bf16x8 p[QB][PROBS][2], one;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) carries |= __builtin_amdgcn_exp2f(top[qb] - ref[qb]) > kFine * sum[qb][0];
-    const bool fine = PROBS == 3 || __any(carries);      // whether the tile's probabilities need more than their first part
-
-    bf16x8 p[QB][PROBS][2];
-    float e[QB][2][8];                          // keys 16 grp + 8 h + 4 i + t; then what their first part leaves
+    for (int i = 0; i < 8; ++i) one[i] = (__bf16)1.f;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        float e[8];                             // keys 16 grp + 8 h + 4 i + t
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) e[qb][h][4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
-        bf16x8 part[1];
-        split_parts<1>(e[qb][h], part);
-        p[qb][0][h] = part[0];
-      }
-    if (fine) {
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+          for (int t = 0; t < 4; ++t) e[4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
           bf16x8 part[PROBS];
-          split_parts<PROBS>(e[qb][h], part);
+          split_parts<PROBS>(e, part);
 #pragma unroll
-          for (int k = PROBS - 1; k > 0; --k) {
-            p[qb][k][h] = part[k];
-            sum[qb] = mfma16(ones, part[k], sum[qb]);
-          }
-        }
-    }
+          for (int k = 0; k < PROBS; ++k) p[qb][k][h] = part[k];
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) sum[qb] = mfma16(ones, p[qb][0][h], sum[qb]);
+        for (int k = PROBS - 1; k >= 0; --k) sum[qb] = mfma16(one, p[qb][k][h], sum[qb]);
+      }
 
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -455,17 +434,12 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
           op[0][x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x05040100u);
           op[1][x] = __builtin_amdgcn_perm(y[2 * x + 1], y[2 * x], 0x07060302u);
         }
-        auto products = [&](int k) {
+#pragma unroll
+        for (int k = PROBS - 1; k >= 0; --k)
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
             for (int j = 0; j < 2; ++j) o[qb][2 * B + j] = mfma16(__builtin_bit_cast(bf16x8, op[j]), p[qb][k][h], o[qb][2 * B + j]);
-        };
-        products(0);
-        if (fine) {
-#pragma unroll
-          for (int k = 1; k < PROBS; ++k) products(k);
-        }
       };
       columns(std::integral_constant<int, 0>());
       columns(std::integral_constant<int, 1>());
@@ -476,22 +450,28 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
     }
     key0 += kStride;
   };
-  // two tiles a turn: the codes of V are on their way a whole tile ahead, each tile's in registers of its own
   if (key0 < key_hi) {
-    ValueCodes<D> even, odd;
+    // the codes of V are on their way a whole tile ahead
     int32_t vp = page_of(a, table, key0 + 16 * grp, key_hi), vp1 = page_of(a, table, key0 + kStride + 16 * grp, key_hi);
+    ValueCodes<D> even, odd;
     load_v<D>(even, pg, kvh, key0, vp, m, grp);
     while (true) {
       int32_t vp2 = page_of(a, table, key0 + 2 * kStride + 16 * grp, key_hi);
       if (key0 + kStride < key_hi) load_v<D>(odd, pg, kvh, key0 + kStride, vp1, m, grp);
       tile(even, vp);
       if (key0 >= key_hi) break;
-      vp = vp2;
-      vp2 = page_of(a, table, key0 + 2 * kStride + 16 * grp, key_hi);
-      if (key0 + kStride < key_hi) load_v<D>(even, pg, kvh, key0 + kStride, vp, m, grp);
-      tile(odd, vp1);
-      if (key0 >= key_hi) break;
-      vp1 = vp2;
+      if constexpr (QB == 2) {                 // two tiles a turn would not fit the registers
+        even = odd;
+        vp = vp1;
+        vp1 = vp2;
+      } else {
+        vp = vp2;
+        vp2 = page_of(a, table, key0 + 2 * kStride + 16 * grp, key_hi);
+        if (key0 + kStride < key_hi) load_v<D>(even, pg, kvh, key0 + kStride, vp, m, grp);
+        tile(odd, vp1);
+        if (key0 >= key_hi) break;
+        vp1 = vp2;
+      }
     }
   }
 
@@ -641,7 +621,7 @@ bool tile_fits(int d) { return d == 64 || d == 128; }
 //  - else as many as bring the launch to the workgroups that are resident at once, two a compute unit: more of them only add their
 //    starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless requests differ in length: those of a
 //    batch of single tokens are cut half as long, so that short ones make room (32 requests of 128 .. 8192 keys: 27 us, without 36).
-struct TilePlan { int tr, rows, slots, splits, chunk, by_request; size_t rows_all; };
+struct TilePlan { int tr, rows, splits, chunk, by_request; int64_t slots; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   TilePlan p{};
   const int64_t most = (int64_t)a.max_new * a.pg.group;
@@ -649,7 +629,7 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   const int tr = p.tr;
   p.by_request = most <= tr;
   p.rows = (int)(most < tr ? most : tr);
-  p.slots = p.by_request ? a.n : (int)((int64_t)a.tokens * a.pg.group / tr) + a.n;
+  p.slots = p.by_request ? a.n : (int64_t)a.tokens * a.pg.group / tr + a.n;
   // tiles that have rows, about
   const int64_t units = (p.by_request ? a.n : ((int64_t)a.tokens * a.pg.group + tr - 1) / tr) * a.pg.Hkv;
   const int64_t keys = a.max_held > 0 ? a.max_held : 1;
@@ -684,6 +664,14 @@ hipError_t launch_tiles(const TileArgs& g, const TilePlan& p, hipStream_t s) {
 
 }  // namespace
 
+bool pages_attn_fits(int dtype, const PagesAttnArgs& a) {
+  const int64_t most = 0x7fffffff;
+  if ((int64_t)a.tokens * a.pg.group > most) return false;
+  if (!tile_fits(a.pg.d)) return true;
+  const TilePlan p = tile_plan(dtype, a);
+  return p.slots * a.pg.Hkv * std::max<int64_t>(p.splits, p.rows) <= most;
+}
+
 size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a) {
   if (!tile_fits(a.pg.d)) return 0;
   const TilePlan p = tile_plan(dtype, a);
@@ -693,7 +681,7 @@ size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a) {
 hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace, hipStream_t s) {
   if (tile_fits(a.pg.d)) {
     const TilePlan p = tile_plan(dtype, a);
-    TileArgs g{a, p.splits, p.chunk, p.slots, p.by_request, (float*)workspace, (float*)workspace + p.rows_all * a.pg.d};
+    TileArgs g{a, p.splits, p.chunk, (int32_t)p.slots, p.by_request, (float*)workspace, (float*)workspace + p.rows_all * a.pg.d};
     if (dtype == LOCOCO_F32) return a.pg.d == 64 ? launch_tiles<float, 64>(g, p, s) : launch_tiles<float, 128>(g, p, s);
     return a.pg.d == 64 ? launch_tiles<__bf16, 64>(g, p, s) : launch_tiles<__bf16, 128>(g, p, s);
   }

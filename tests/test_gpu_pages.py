@@ -422,3 +422,26 @@ def test_attention_of_many_requests(n, group):
     lens[n // 2], lens[-1] = (90, 75 if group == 1 else 5), (33, 4)
     batch = make_batch(81, torch.bfloat16, 1, group, 64, 16, lens)
     check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+@pytest.mark.parametrize("span", [3, 12, 40])
+def test_attention_with_values_of_all_sizes(dtype, d, span):
+    """Rows of V whose sizes differ by up to 2^80, a row of zeros among them, in ascending, descending and any order: a row's result may hang
+    on a key that its probabilities hardly show."""
+    lens = [(300, 1), (600, 40), (97, 5), (700, 1)]
+    pages, q, tables, starts, held = make_batch(91, dtype, 2, 2, d, 16, lens)
+    g = torch.Generator().manual_seed(span)
+    scales = pages.v_scales.cpu()
+    for i, (h, _) in enumerate(lens):
+        size = torch.randint(-span, span + 1, (h,), generator=g)
+        size = [size, size.sort().values, size.sort(descending=True).values, size][i]
+        for j in range(h):
+            page, row = int(tables[i, j // 16]), j % 16
+            scales[page, :, :, row] = 27 if j == h // 3 else (scales[page, :, :, row].int() + int(size[j])).to(torch.uint8)
+            if j == h // 3:
+                pages.v_codes[page, :, row] = 0
+    pages.v_scales.copy_(scales)
+    batch = (pages, q, tables, starts, held)
+    check_attn(*batch, run_attn(*batch))
