@@ -472,7 +472,8 @@ typedef struct lococo_requests {
   int32_t table_pages;    /* entries of a table; table_pages * page_rows < 2^30                              */
   int32_t max_new;        /* no request has more new rows, of those it is the caller's promise: what is over
                              is left unwritten                                                               */
-  int32_t max_held;       /* about the most rows a request holds: only how the work is dealt out goes by it  */
+  int32_t max_held;       /* about the most rows a request holds: how the work is dealt out, and with it the
+                             order of fp32 sums, goes by it, nothing else                                    */
   const int32_t* tables;  /* device [n][table_pages]                                                         */
   const int32_t* starts;  /* device [n + 1], not decreasing: request i's queries are rows starts[i] ..       */
   const int32_t* held;    /* device [n]: rows held, the new ones among them (the plan's held_after)          */
@@ -484,6 +485,7 @@ typedef struct lococo_requests {
  * that no request has are not written, rows whose table entry is no page are left out.  q and o: [b, n_q_heads, rows_per_batch,
  * head_dim] views of requests->tokens rows counted as in lococo_pages_store; o must not alias q.  Softmax and sums in fp32,
  * operands as stored; probabilities enter their product with 16 bits or more for LOCOCO_BF16, with all 24 for LOCOCO_F32.  A visible row's NaN reaches the results of the queries that see it and no others.
+ * Identical calls return the same bits.  head_dim 64 and 128 run on the matrix cores, others on vector arithmetic, a wave a row.
  * workspace: device, 256-byte aligned, lococo_pages_workspace_bytes of the same sizes, or of a larger max_held (may be 0). */
 LOCOCO_API lococo_status lococo_pages_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out);
 LOCOCO_API lococo_status lococo_pages_attn(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,

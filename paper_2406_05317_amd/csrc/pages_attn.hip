@@ -115,7 +115,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// head_dim 64 and 128: matrix instructions.  A workgroup takes kRows = 16 QB query rows that share a kv head (the new rows of a request
+// head_dim 64 and 128: matrix instructions.  A workgroup takes TR = 16 QB query rows that share a kv head (the new rows of a request
 // times the heads of the group) and a part of the keys; its four waves take the 64-key tiles of that part in turn, each for all the
 // query rows with a running softmax of its own, and meet once, at the end.  No wave waits for another before that, nothing passes
 // through LDS on the way: codes go from memory to operand registers.
@@ -134,6 +134,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 // but is off by as much as the rounding of a bf16 result wherever one key carries a column, be it by its probability or, as where new
 // rows stand beside the averages of a compressed memory, by the size of its value.  Their sum is taken of the same numbers, by a product
 // with ones: no vector instruction adds.
+//
+// Bound, single tokens: by memory and by the start and end of a workgroup, some 7 us: 131072 keys of 8 heads, 143 MB, 28.5 us of which
+// (5.0 TB/s) beside the join's 4.  Many rows: by the instructions around 104 MFMAs a tile of 64 keys x 32 rows: 3349 tokens on up to 14 K
+// keys of 32 heads 0.99 ms, 686 TFLOP/s of 4 d flops a pair.  Each wave keeps the codes of V a whole tile ahead; the codes of K for the next
+// tile go into the registers the scores have just been taken from.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
 

@@ -2,7 +2,7 @@
 (equal), attention over the pages.
 
 Tolerances of the attention, per element, from the arithmetic the header promises: with A = sum p |v|,
-  bf16: probabilities and the result are rounded to 8 bits: 2^-9 A each; the fp32 part below them
+  bf16: the result is rounded to 8 bits, 2^-8 A at most (probabilities enter with 16 bits); the fp32 part below beside it
   both: a score's error is at most (d + 8) 2^-23 sum |q k| scale (products exact or rounded once, d additions, the factor), and as much
         again for the argument of the exponential; p takes it twice (itself and the sum); the sums of up to n terms: (n + 64) 2^-23 A."""
 import math
