@@ -564,6 +564,14 @@ __global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t row
     const int32_t mine = k0 + l * WAVES, n = min((parts - k0 + WAVES - 1) / WAVES, 64);
     const bool real = mine < parts;
     const f32x2 st = real ? *(const f32x2*)(g.part_ml + 2 * (pr + (int64_t)mine * TR)) : f32x2{kNoRef, 0.f};
+    // eight parts' columns on their way at once, the first ones beside the references; what is over is the last part times a lane's 0
+    const float* at = g.part_o + (pr + (int64_t)k0 * TR) * D + l * (D / 64);
+    auto load = [&](int32_t k, cols (&v)[8]) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = *(const cols*)(at + (int64_t)min(k + j, n - 1) * WAVES * TR * D);
+    };
+    cols v[8];
+    load(0, v);
     float top = st[0];
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
@@ -575,11 +583,8 @@ __global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t row
     total = total * keep + sum;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) y[i] *= keep;
-    const float* at = g.part_o + (pr + (int64_t)k0 * TR) * D + l * (D / 64);
-    for (int32_t k = 0; k < n; k += 8) {         // eight parts on their way at once; what is over is the last one times the 0 of a lane
-      cols v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = *(const cols*)(at + (int64_t)min(k + j, n - 1) * WAVES * TR * D);
+    for (int32_t k = 0; k < n; k += 8) {
+      if (k) load(k, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float fk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + j));
