@@ -130,15 +130,15 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 //
 // Running softmax: the reference a row's exponentials are taken against moves only when a tile's largest score passes it by 8 (in powers
 // of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits), for fp32
-// rows of three (all 24 bits), as their queries do.  One alone would save a third of the MFMAs (prompts of 2000 tokens 0.81 ms for 0.99),
+// rows of three (all 24 bits), as their queries do.  One alone would save a third of the MFMAs (prompts of 2000 tokens 0.81 ms for 0.99 then),
 // but is off by as much as the rounding of a bf16 result wherever one key carries a column, be it by its probability or, as where new
 // rows stand beside the averages of a compressed memory, by the size of its value.  Their sum is taken of the same numbers, by a product
 // with ones: no vector instruction adds.
 //
-// Bound, single tokens: by memory and by the start and end of a workgroup, some 7 us: 131072 keys of 8 heads, 143 MB, 28.5 us of which
-// (5.0 TB/s) beside the join's 4.  Many rows: by the instructions around 104 MFMAs a tile of 64 keys x 32 rows: 3349 tokens on up to 14 K
-// keys of 32 heads 0.99 ms, 686 TFLOP/s of 4 d flops a pair.  Each wave keeps the codes of V a whole tile ahead; the codes of K for the next
-// tile go into the registers the scores have just been taken from.
+// Bound, single tokens: by memory and by the start and end of a workgroup, some 7 us: 131072 keys of 8 heads, 143 MB, 27.6 us
+// (5.1 TB/s), and 4 for the join.  Many rows: by the instructions around 104 MFMAs a tile of 64 keys x 32 rows (vector port 68 % busy,
+// matrix pipe 44 %): 3349 tokens on up to 14 K keys of 32 heads 0.97 - 1.01 ms, 670 - 700 TFLOP/s of 4 d flops a pair.  Each wave asks
+// for the codes of V a whole tile ahead; those of K for the next tile go into the registers the scores have just been taken from.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
 
@@ -344,6 +344,9 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
   kp = page_of(a, table, key0 + kStride + 4 * m, key_hi);
   // one tile: vp is the page of a lane's keys
   auto tile = [&](const ValueCodes<D>& vc, int32_t vp) {
+    // a wave in either product goes ahead of one in its softmax: the matrix pipe is given work while vector instructions wait (prompts
+    // 1 to 2 % shorter, 77 tokens on 3 K keys 4 to 6 %)
+    __builtin_amdgcn_s_setprio(1);
     f4 s[QB][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -381,6 +384,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         if (!in || odd) vs[x / 4] &= ~(255u << (8 * (x % 4)));
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     float top[QB];
     bool grown = false;
 #pragma unroll
@@ -423,6 +427,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         for (int k = PROBS - 1; k >= 0; --k) sum[qb] = mfma16(one, p[qb][k][h], sum[qb]);
       }
 
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float sc[8];
@@ -453,6 +458,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         columns(std::integral_constant<int, 3>());
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     key0 += kStride;
   };
   if (key0 < key_hi) {
