@@ -646,8 +646,8 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   p.by_request = most <= tr;
   p.rows = (int)(most < tr ? most : tr);
   p.slots = p.by_request ? a.n : (int64_t)a.tokens * a.pg.group / tr + a.n;
-  // tiles that have rows, about
-  const int64_t units = (p.by_request ? a.n : ((int64_t)a.tokens * a.pg.group + tr - 1) / tr) * a.pg.Hkv;
+  // tiles that have rows, about (one at least: a call without rows asks for its workspace as well)
+  const int64_t units = (p.by_request ? a.n : std::max<int64_t>(((int64_t)a.tokens * a.pg.group + tr - 1) / tr, 1)) * a.pg.Hkv;
   const int64_t keys = a.max_held > 0 ? a.max_held : 1;
   constexpr int64_t kLeast = kTileWaves * kTileKeys;
   // not fewer parts for more keys: a workspace for many takes fewer

@@ -4,6 +4,7 @@ import os
 import re
 import shutil
 import subprocess
+import sys
 
 import pytest
 
@@ -95,6 +96,30 @@ def test_calls_of_no_rows_do_nothing():
     assert L.lococo_pages_store(C.byref(p), C.byref(none), C.byref(none), 1, 0, None, None) == lb.LOCOCO_OK
     assert L.lococo_pages_load(C.byref(p), None, 1, 0, C.byref(none), C.byref(none), None) == lb.LOCOCO_OK
     assert L.lococo_pages_attn(C.byref(p), C.byref(requests(tokens=0, max_new=0)), C.byref(none), C.byref(none), 1, None, 0, None) == lb.LOCOCO_OK
+
+
+IDLE = """
+import ctypes as C, sys
+sys.path.insert(0, sys.argv[1])
+from test_pages_cpu import FAKE, lb, pages, requests, tensor
+L, none, out = lb.lib(), tensor(None), C.c_size_t(0)
+for dtype in (lb.LOCOCO_F32, lb.LOCOCO_BF16):
+    for d in (64, 96, 128):
+        for max_new in (0, 1, 9, 77):
+            for max_held in (0, 300, 769, 4096, 131072):
+                p, r = pages(dtype=dtype, head_dim=d), requests(tokens=0, max_new=max_new, max_held=max_held, table_pages=3000)
+                st = L.lococo_pages_workspace_bytes(C.byref(p), C.byref(r), C.byref(out))
+                st |= L.lococo_pages_attn(C.byref(p), C.byref(r), C.byref(none), C.byref(none), 1, None, 0, None)
+                assert st == lb.LOCOCO_OK, (dtype, d, max_new, max_held, st)
+print("every idle turn returned")
+"""
+
+
+def test_idle_turns_do_nothing_whatever_they_promise():
+    """No rows, with max_new and max_held as a server's busier turns have them (in a process of its own: an arithmetic trap would end it)."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", IDLE, here], capture_output=True, text=True, timeout=300, cwd=os.path.dirname(here))
+    assert r.returncode == 0 and "every idle turn returned" in r.stdout, (r.returncode, r.stderr[-2000:])
 
 
 def test_workspace_does_not_shrink_with_more_keys():
