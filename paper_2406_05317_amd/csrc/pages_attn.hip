@@ -159,24 +159,30 @@ struct TileJob {
   int32_t keys;                                // keys its last row sees
 };
 
+// The slot request i's tiles begin at.  A request with rows opens one tile more than its whole ones at most, and moves min(i, starts) on by
+// one at least: its tiles never reach into the next one's.  Requests without rows, of which there may be thousands, take no slot.
+template <int TR>
+__device__ __forceinline__ int32_t first_slot(const PagesAttnArgs& a, int32_t i) {
+  const int32_t at = a.starts[i];
+  return (int32_t)((int64_t)at * a.pg.group / TR) + min(i, at);
+}
+
 template <int TR>
 __device__ __forceinline__ bool tile_job(const TileArgs& g, int32_t slot, TileJob* j) {
   const PagesAttnArgs& a = g.a;
   int32_t req = slot, tile = 0;
   if (!g.by_request) {
-    // request i's tiles begin at slot starts[i] * group / TR + i: with that a request's tiles never reach into the next one's.  The last
-    // request that begins at or before the slot, 64 candidates at a look (one trip to memory, two with more than 64 requests).
+    // the last request that begins at or before the slot, 64 candidates at a look (one trip to memory, two with more than 64 requests)
     const int l = threadIdx.x & 63;
     req = 0;
 #pragma unroll
     for (int step = 64; step; step = step == 64 ? 1 : 0) {
       if (step == 64 && a.n <= 64) continue;
-      const int i = min(req + l * step, a.n - 1);
-      const int32_t at = (int32_t)((int64_t)a.starts[i] * a.pg.group / TR) + i;
+      const int32_t at = first_slot<TR>(a, min(req + l * step, a.n - 1));
       req += max(__popcll(__ballot(req + l * step < a.n && at <= slot)) - 1, 0) * step;
     }
     req = __builtin_amdgcn_readfirstlane(req);
-    tile = slot - (int32_t)((int64_t)a.starts[req] * a.pg.group / TR) - req;
+    tile = slot - first_slot<TR>(a, req);
     if (tile < 0) return false;
   }
   j->req = req;
@@ -637,6 +643,7 @@ bool tile_fits(int d) { return d == 64 || d == 128; }
 //  - else as many as bring the launch to the workgroups that are resident at once, two a compute unit: more of them only add their
 //    starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless requests differ in length: those of a
 //    batch of single tokens are cut half as long, so that short ones make room (32 requests of 128 .. 8192 keys: 27 us, without 36).
+constexpr int kPartTiles = 8;                  // a workspace holds parts of so many times the tiles that are resident: 68 MB at d = 128
 struct TilePlan { int tr, rows, splits, chunk, by_request; int64_t slots; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   TilePlan p{};
@@ -645,7 +652,7 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   const int tr = p.tr;
   p.by_request = most <= tr;
   p.rows = (int)(most < tr ? most : tr);
-  p.slots = p.by_request ? a.n : (int64_t)a.tokens * a.pg.group / tr + a.n;
+  p.slots = p.by_request ? a.n : (int64_t)a.tokens * a.pg.group / tr + std::min(a.n, a.tokens);     // (first_slot)
   // tiles that have rows, about (one at least: a call without rows asks for its workspace as well)
   const int64_t units = (p.by_request ? a.n : std::max<int64_t>(((int64_t)a.tokens * a.pg.group + tr - 1) / tr, 1)) * a.pg.Hkv;
   const int64_t keys = a.max_held > 0 ? a.max_held : 1;
@@ -653,7 +660,11 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   // not fewer parts for more keys: a workspace for many takes fewer
   const int64_t resident = 2 * (int64_t)cu_count(), target = p.by_request && a.n > 1 && units < resident ? 2 * resident : resident;
   const int64_t whole = 2 * units >= resident ? 2048 : 768;
-  const int64_t want = keys <= whole ? 1 : std::max<int64_t>(target / units, 1), splits = std::min(want, (keys + kLeast - 1) / kLeast);
+  // slots may be more than tiles: parts lie in the workspace by slot, and what they take there is bounded (two requests of 33 and 7 rows
+  // on 131072 keys among 510 without rows, 8 kv heads: 66 MB and 263 us; bounded at a quarter of that, 705 us)
+  const int64_t room = kPartTiles * resident / std::max<int64_t>(p.slots * a.pg.Hkv, 1);
+  const int64_t want = keys <= whole ? 1 : std::max<int64_t>(std::min(target / units, room), 1);
+  const int64_t splits = std::min(want, (keys + kLeast - 1) / kLeast);
   p.splits = (int)splits;
   p.chunk = (int)std::max<int64_t>(kLeast, ((keys + splits - 1) / splits + kTileKeys - 1) / kTileKeys * kTileKeys);
   p.rows_all = (size_t)p.slots * a.pg.Hkv * p.splits * tr;

@@ -445,3 +445,16 @@ def test_attention_with_values_of_all_sizes(dtype, d, span):
     pages.v_scales.copy_(scales)
     batch = (pages, q, tables, starts, held)
     check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,group", [(40, 4), (130, 1), (700, 4), (700, 20)])
+@pytest.mark.parametrize("first", [0, 1])
+def test_attention_where_most_requests_are_idle(dtype, n, group, first):
+    """A few requests with new rows and long contexts, in several parts, among many without: ahead of them, between them, behind them."""
+    lens = [(7, 0)] * n
+    for i, busy in zip((first * 3, n // 3, n // 3 + 1, n - 1 - first * 5), ((1500, 35), (2300, 1), (12, 17), (900, 40))):
+        lens[i] = busy
+    batch = make_batch(101, dtype, 1, group, 64, 16, lens)
+    print(dtype, n, group, first, flush=True)
+    check_attn(*batch, run_attn(*batch))

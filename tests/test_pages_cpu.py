@@ -134,6 +134,21 @@ def test_workspace_does_not_shrink_with_more_keys():
             last = out.value
 
 
+@pytest.mark.parametrize("n,tokens,max_new", [(512, 40, 33), (4096, 64, 64), (4096, 4, 9), (4096, 4, 33), (300, 1055, 1024), (64, 127, 64),
+                                              (4096, 4096, 2), (700, 50, 17), (1, 77, 77), (32, 32, 1)])
+@pytest.mark.parametrize("kv,group", [(8, 4), (32, 1), (1, 1), (4, 8), (1, 64)])
+@pytest.mark.parametrize("dtype,d", [(lb.LOCOCO_BF16, 128), (lb.LOCOCO_F32, 128), (lb.LOCOCO_BF16, 64)])
+def test_workspace_is_bounded_by_what_is_resident(n, tokens, max_new, kv, group, dtype, d):
+    """Parts of the keys are for calls that leave the device idle.  Two workgroups to each of 256 compute units are resident: however many
+    requests of a call are idle, the parts of eight times as many tiles of 32 rows are room enough."""
+    L, out = lb.lib(), C.c_size_t(0)
+    p = pages(dtype=dtype, n_q_heads=kv * group, n_kv_heads=kv, head_dim=d)
+    for held in (1000, 5000, 131072, 2 ** 30):
+        r = requests(n=n, tokens=tokens, max_new=max_new, max_held=held)
+        assert L.lococo_pages_workspace_bytes(C.byref(p), C.byref(r), C.byref(out)) == lb.LOCOCO_OK
+        assert out.value <= 8 * 512 * 32 * (d + 2) * 4, held
+
+
 def test_plan_arguments_are_checked():
     L, p = lb.lib(), pages(k_codes=None, dtype=9)                       # the plan reads neither the arrays nor the heads
     names = ["new", "held", "tables", "ring", "ends", "held_after", "ends_after", "starts", "slots", "positions", "totals"]
