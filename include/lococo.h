@@ -485,7 +485,9 @@ typedef struct lococo_requests {
  * that no request has are not written, rows whose table entry is no page are left out.  q and o: [b, n_q_heads, rows_per_batch,
  * head_dim] views of requests->tokens rows counted as in lococo_pages_store; o must not alias q.  Softmax and sums in fp32,
  * operands as stored; probabilities enter their product with 16 bits or more for LOCOCO_BF16, with all 24 for LOCOCO_F32.  A
- * visible row's NaN reaches the results of the queries that see it and no others.  Identical calls return the same bits.
+ * visible row's NaN reaches the results of the queries that see it and no others.  Sums are divided at the end, by then over
+ * exponentials of 1 at most: results are finite where the sum of a column's magnitudes over the visible rows is.  Identical calls return
+ * the same bits.
  * head_dim 64 and 128 run on the matrix cores, others on vector arithmetic, a wave a row.
  * workspace: device, 256-byte aligned, lococo_pages_workspace_bytes of the same sizes, or of a larger max_held (may be 0). */
 LOCOCO_API lococo_status lococo_pages_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out);

@@ -128,8 +128,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 //     step c.  Its other operand, V^T, wants in lane (column, g) those keys' values of one column: lane (m, g) loads, for its 16 keys,
 //     the D/32 bytes of columns D/16 m .. + D/16 - 1 and pairs two keys' values of a column after the conversion.
 //
-// Running softmax: the reference a row's exponentials are taken against moves only when a tile's largest score passes it by 8 (in powers
-// of two), exact after the final division.  Probabilities enter their product as the sum of two bf16 numbers (16 bits), for fp32
+// Running softmax: the reference a row's exponentials are taken against is set 8 (in powers of two) above a tile's largest score and moves
+// only when a later one passes it, exact after the final division: no exponential exceeds 1, and what they weigh, up to 6 * 2^125, does
+// not leave fp32 by them.  Probabilities enter their product as the sum of two bf16 numbers (16 bits), for fp32
 // rows of three (all 24 bits), as their queries do.  One alone would save a third of the MFMAs (prompts of 2000 tokens 0.81 ms for 0.99 then),
 // but is off by as much as the rounding of a bf16 result wherever one key carries a column, be it by its probability or, as where new
 // rows stand beside the averages of a compressed memory, by the size of its value.  Their sum is taken of the same numbers, by a product
@@ -141,6 +142,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
 // for the codes of V a whole tile ahead; those of K for the next tile go into the registers the scores have just been taken from.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
+constexpr float kRefAhead = 8.f;               // of a row's reference over the scores it was taken from
 
 typedef __attribute__((ext_vector_type(4))) float f4;
 
@@ -401,12 +403,12 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) top[qb] = fmaxf(top[qb], s[qb][t][i]);
       top[qb] *= c;
-      grown |= top[qb] > ref[qb] + 8.f;
+      grown |= top[qb] > ref[qb];
     }
     if (__any(grown)) {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        const float next = fmaxf(ref[qb], max_groups(top[qb])), keep = __builtin_amdgcn_exp2f(ref[qb] - next);
+        const float next = fmaxf(ref[qb], max_groups(top[qb]) + kRefAhead), keep = __builtin_amdgcn_exp2f(ref[qb] - next);
         ref[qb] = next;
         sum[qb] = f4{sum[qb][0] * keep, sum[qb][1] * keep, sum[qb][2] * keep, sum[qb][3] * keep};
 #pragma unroll

@@ -458,3 +458,30 @@ def test_attention_where_most_requests_are_idle(dtype, n, group, first):
     batch = make_batch(101, dtype, 1, group, 64, 16, lens)
     print(dtype, n, group, first, flush=True)
     check_attn(*batch, run_attn(*batch))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+@pytest.mark.parametrize("lens", [[(600, 1)], [(3001, 1), (700, 1)], [(600, 20), (2500, 40)], [(330, 2)] * 3])
+def test_attention_with_the_largest_values(dtype, d, lens):
+    """The largest value that rows in 4 bits can have, 6 * 2^125, beside ordinary ones, at a key whose probability exceeds those ahead of it
+    by e^4: what is summed up stays within fp32."""
+    pages, q, tables, starts, held = make_batch(121, dtype, 1, 2, d, 16, lens)
+    pages.c.attn_scale = 1.0
+    q.zero_()
+    q[..., 0] = 1.0
+    for codes, scales in ((pages.k_codes, pages.k_scales), (pages.v_codes, pages.v_scales)):
+        if codes is pages.k_codes:
+            codes.zero_()
+            scales.masked_fill_(scales != 255, 127)
+        for i, (h, w) in enumerate(lens):
+            page, row = int(tables[i, (h - w) // 16]), (h - w) % 16    # the first new row: every query sees it
+            if codes is pages.k_codes:
+                codes[page, :, row, 0] = 6                             # a score of 4, the others' are 0
+            else:
+                codes[page, :, row] = torch.randint(0, 256, (d // 2,), generator=torch.Generator().manual_seed(i)).to(torch.uint8).cuda()
+                scales[page, :, :, row] = 252
+    batch = (pages, q, tables, starts, held)
+    got = run_attn(*batch)
+    assert torch.isfinite(got[:, :, :starts[-1]]).all()
+    check_attn(*batch, got, scale=1.0)
