@@ -31,8 +31,8 @@ __global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnAr
   const int32_t token = blockIdx.x * kRowsWaves + w, h = blockIdx.y, kvh = h / pg.group;
   if (token >= a.tokens) return;                 // nothing below meets the other waves
   const int req = request_of(a.starts, a.n, token);
-  const int32_t stop = a.starts[req + 1];
-  if (token >= stop) return;                     // behind the last request
+  const int32_t stop = min(a.starts[req + 1], a.tokens);
+  if (token < a.starts[req] || token >= stop) return;                       // nobody's: ahead of the first request, behind the last
   const int32_t held = min(max(a.held[req], 0), a.table_pages << pg.page_shift);
   const int32_t seen = max(held - (stop - token) + 1, 0);                   // rows the query sees
   const int32_t b = token / a.q.t, t = token - b * a.q.t;

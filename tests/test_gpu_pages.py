@@ -485,3 +485,21 @@ def test_attention_with_the_largest_values(dtype, d, lens):
     got = run_attn(*batch)
     assert torch.isfinite(got[:, :, :starts[-1]]).all()
     check_attn(*batch, got, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,d", [(2, 64), (2, 128), (2, 96), (1, 160)])
+@pytest.mark.parametrize("lens", [[(50, 1), (7, 1), (130, 1)], [(900, 40), (30, 3)]])
+def test_attention_leaves_rows_ahead_of_the_first_request(dtype, group, d, lens):
+    """Requests whose rows begin behind the call's first ones, which belong to nobody."""
+    ahead = 5
+    pages, q, tables, starts, held = make_batch(111, dtype, 1, group, d, 16, lens)
+    want = run_attn(pages, q, tables, starts, held)
+    check_attn(pages, q, tables, starts, held, want)
+    o = torch.full((1, group, ahead + q.shape[2], d), 3.0, dtype=dtype, device="cuda")
+    most = max(w for _, w in lens) + ahead                             # (enough for max_new * n to cover the call's rows)
+    ws = lb.pages_workspace(pages, len(lens), o.shape[2], most, int(held.max()))
+    lb.lococo_pages_attn(pages, torch.cat((q[:, :, :1].expand(-1, -1, ahead, -1), q), 2).cuda(), o, tables.cuda(), (starts + ahead).cuda(),
+                         held.cuda(), most, int(held.max()), ws)
+    assert (o[:, :, :ahead] == 3).all()
+    check_attn(pages, q, tables, starts, held, o[:, :, ahead:])
