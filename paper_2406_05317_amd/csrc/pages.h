@@ -66,7 +66,7 @@ hipError_t launch_pages_store(int dtype, const PagesView& pg, const RowsView& k,
 hipError_t launch_pages_load(int dtype, const PagesView& pg, const RowsView& k, const RowsView& v, int32_t tokens,
                              const int32_t* slots, hipStream_t s);
 // ---- pages_attn.hip
-bool pages_attn_fits(int dtype, const PagesAttnArgs& a);     // the launch's indices are 32 bits
+bool pages_attn_fits(int dtype, const PagesAttnArgs& a);     // a launch takes the work
 size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a);
 hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace, hipStream_t s);
 

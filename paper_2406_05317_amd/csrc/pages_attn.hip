@@ -20,10 +20,10 @@ __device__ __forceinline__ int request_of(const int32_t* starts, int n, int32_t 
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Any head_dim that is a multiple of 32: a wave to a query row, a lane to a key, vector arithmetic in fp32.
-constexpr int kRowsWaves = 4;
+constexpr int kRowsWaves = 4, kRowsThreads = 64 * kRowsWaves;
 
 template <typename T>
-__global__ __launch_bounds__(64 * kRowsWaves) void pages_attn_rows_k(PagesAttnArgs a) {
+__global__ __launch_bounds__(kRowsThreads) void pages_attn_rows_k(PagesAttnArgs a) {
   __shared__ float qs[kRowsWaves][kPagesMaxHeadDim], ps[kRowsWaves][64];
   __shared__ int64_t at[kRowsWaves][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -635,6 +635,9 @@ __global__ __launch_bounds__(256) void pages_attn_join_k(TileArgs g, int32_t row
   for (int i = 0; i < D / 64; ++i) out[i] = (T)(y[i] * inv);
 }
 
+constexpr int64_t kLaunchThreads = 0xffffffffll;                            // of a launch's dimension at most
+int64_t rows_groups(int32_t tokens) { return ((int64_t)tokens + kRowsWaves - 1) / kRowsWaves; }
+
 bool tile_fits(int d) { return d == 64 || d == 128; }
 
 // How the work is dealt out.  Row tiles of 32 where a request has more than 16 rows (new rows times the group) and rows are bf16.
@@ -673,13 +676,20 @@ TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
   return p;
 }
 
+constexpr int kTileThreads = 64 * kTileWaves, kJoinThreads = 256;
+// workgroups of the two launches; the join takes a row with a wave, or with four where there are many parts
+int64_t tile_groups(const TilePlan& p, int Hkv) { return p.slots * Hkv * p.splits; }
+int64_t join_groups(const TilePlan& p, int Hkv) {
+  return p.splits == 1 ? 0 : p.slots * Hkv * (p.splits > 16 ? p.rows : (p.rows + 3) / 4);
+}
+
 template <typename T, int D, int TR>
 hipError_t launch_tile(const TileArgs& g, const TilePlan& p, hipStream_t s) {
-  const unsigned tiles = (unsigned)p.slots * (unsigned)g.a.pg.Hkv, grid = tiles * (unsigned)p.splits, rows = (unsigned)p.rows;
-  pages_attn_tile_k<T, D, TR / 16><<<grid, 64 * kTileWaves, 0, s>>>(g);
-  if (p.splits > 1) {
-    if (p.splits > 16) pages_attn_join_k<T, D, TR, 4><<<tiles * rows, 256, 0, s>>>(g, p.rows);
-    else pages_attn_join_k<T, D, TR, 1><<<tiles * ((rows + 3) / 4), 256, 0, s>>>(g, p.rows);
+  const unsigned join = (unsigned)join_groups(p, g.a.pg.Hkv);
+  pages_attn_tile_k<T, D, TR / 16><<<(unsigned)tile_groups(p, g.a.pg.Hkv), kTileThreads, 0, s>>>(g);
+  if (join) {
+    if (p.splits > 16) pages_attn_join_k<T, D, TR, 4><<<join, kJoinThreads, 0, s>>>(g, p.rows);
+    else pages_attn_join_k<T, D, TR, 1><<<join, kJoinThreads, 0, s>>>(g, p.rows);
   }
   return hipGetLastError();
 }
@@ -694,11 +704,10 @@ hipError_t launch_tiles(const TileArgs& g, const TilePlan& p, hipStream_t s) {
 }  // namespace
 
 bool pages_attn_fits(int dtype, const PagesAttnArgs& a) {
-  const int64_t most = 0x7fffffff;
-  if ((int64_t)a.tokens * a.pg.group > most) return false;
-  if (!tile_fits(a.pg.d)) return true;
+  if ((int64_t)a.tokens * a.pg.group > 0x7fffffff) return false;             // rows of a kv head are counted in 32 bits
+  if (!tile_fits(a.pg.d)) return rows_groups(a.tokens) * kRowsThreads <= kLaunchThreads;
   const TilePlan p = tile_plan(dtype, a);
-  return p.slots * a.pg.Hkv * std::max<int64_t>(p.splits, p.rows) <= most;
+  return tile_groups(p, a.pg.Hkv) * kTileThreads <= kLaunchThreads && join_groups(p, a.pg.Hkv) * kJoinThreads <= kLaunchThreads;
 }
 
 size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a) {
@@ -714,9 +723,9 @@ hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace,
     if (dtype == LOCOCO_F32) return a.pg.d == 64 ? launch_tiles<float, 64>(g, p, s) : launch_tiles<float, 128>(g, p, s);
     return a.pg.d == 64 ? launch_tiles<__bf16, 64>(g, p, s) : launch_tiles<__bf16, 128>(g, p, s);
   }
-  const dim3 grid((unsigned)((a.tokens + kRowsWaves - 1) / kRowsWaves), (unsigned)a.pg.Hq);
-  if (dtype == LOCOCO_F32) pages_attn_rows_k<float><<<grid, 64 * kRowsWaves, 0, s>>>(a);
-  else pages_attn_rows_k<__bf16><<<grid, 64 * kRowsWaves, 0, s>>>(a);
+  const dim3 grid((unsigned)rows_groups(a.tokens), (unsigned)a.pg.Hq);
+  if (dtype == LOCOCO_F32) pages_attn_rows_k<float><<<grid, kRowsThreads, 0, s>>>(a);
+  else pages_attn_rows_k<__bf16><<<grid, kRowsThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

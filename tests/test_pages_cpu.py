@@ -170,6 +170,20 @@ def test_plan_arguments_are_checked():
     assert plan(pg=pages(page_rows=24)) == lb.LOCOCO_EUNSUPPORTED
 
 
+@pytest.mark.parametrize("over,fit", [                                   # a launch's dimension has fewer than 2^32 threads: 2^24 workgroups of 256
+    (dict(head_dim=128, n_q_heads=32, n_kv_heads=32), 32 * (2 ** 19 - 2) + 31),               # 32 rows a workgroup, 32 kv heads, one spare tile
+    (dict(head_dim=64, n_q_heads=32, n_kv_heads=32, dtype=lb.LOCOCO_F32), 16 * (2 ** 19 - 2) + 15),
+    (dict(head_dim=128, n_q_heads=128, n_kv_heads=64), 16 * (2 ** 18 - 2) + 15),              # two rows a token
+    (dict(head_dim=96, n_q_heads=1, n_kv_heads=1), 4 * (2 ** 24 - 1)),                        # 4 rows a workgroup
+    (dict(head_dim=256, n_q_heads=8, n_kv_heads=2), 4 * (2 ** 24 - 1))])
+def test_attention_takes_what_a_launch_takes(over, fit):
+    L, p, out = lb.lib(), pages(**over), C.c_size_t(0)
+    size = lambda tokens: L.lococo_pages_workspace_bytes(C.byref(p), C.byref(requests(n=1, tokens=tokens, max_new=tokens)), C.byref(out))
+    assert size(fit) == lb.LOCOCO_OK and size(fit + 1) == lb.LOCOCO_EUNSUPPORTED
+    assert L.lococo_pages_attn(C.byref(p), C.byref(requests(n=1, tokens=fit + 1, max_new=fit + 1)), C.byref(tensor()), C.byref(tensor(FAKE[9])),
+                               fit + 1, None, 0, None) == lb.LOCOCO_EUNSUPPORTED
+
+
 @pytest.mark.skipif(shutil.which("hipcc") is None, reason="needs hipcc")
 def test_attention_kernels_keep_everything_in_registers(tmp_path):
     """A reload from scratch memory waits for every load on its way: the codes requested a tile ahead (with 6 registers there the kernel of
