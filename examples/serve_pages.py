@@ -37,20 +37,26 @@ class Requests:
         self.tables = torch.full((n, per), -1, **i32)
         self.held, self.starts, self.totals = torch.zeros(n, **i32), torch.zeros(n + 1, **i32), torch.zeros(4, **i32)
         self.next_held, self.next_ends = torch.zeros_like(self.held), torch.zeros_like(self.ends)
+        self.sums = torch.zeros(4, dtype=torch.int64, device="cuda")    # over all turns: rows placed, pages taken, given back, refusals
         self.longest = 0                                # what the host knows of the lengths: enough to deal out the work
 
     def plan(self, new_rows: torch.Tensor, tokens: int, max_new: int):
-        """Places new_rows[i] rows (-1: request i ends) of every request; returns the slots and positions of the call's `tokens` rows."""
+        """Places new_rows[i] rows (-1: request i ends) of every request; returns the slots and positions of the call's `tokens` rows.  The
+        rows of a request that was refused, its table or the pool being full, have no slots (-1)."""
         slots, positions = (torch.empty(tokens, dtype=torch.int32, device="cuda") for _ in range(2))
         lb.lococo_pages_plan(self.pages, new_rows, self.held, self.tables, self.ring, self.ends, self.next_held, self.next_ends, self.starts,
                              slots, positions, self.totals)
         self.held, self.next_held = self.next_held, self.held
         self.ends, self.next_ends = self.next_ends, self.ends
         self.longest = min(self.longest + max_new, self.most)
+        self.slots = slots
+        self.sums += self.totals                        # (on the device, as everything here)
         return slots, positions
 
     def attend(self, q, o, max_new: int, workspace):
+        """Attention of the planned rows; zeros for those of refused requests, whose attention has no meaning."""
         lb.lococo_pages_attn(self.pages, q, o, self.tables, self.starts, self.held, max_new, self.longest, workspace)
+        o.masked_fill_((self.slots < 0).view(q.shape[0], 1, q.shape[2], 1), 0)
 
     def workspace(self, tokens: int, max_new: int):
         return lb.pages_workspace(self.pages, self.n, tokens, max_new, self.most)
@@ -64,7 +70,7 @@ def compress(prompt_k, prompt_v, q, filters):
     return cache.k, cache.v, cache.len
 
 
-def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None) -> dict:
+def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None, rows_each: int = 4096) -> dict:
     """Runs the requests; on_turn(what, requests, q, k, v, o) is called behind every attention (tests look in there)."""
     g = torch.Generator(device="cuda").manual_seed(seed)
 
@@ -72,7 +78,7 @@ def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None) -> dict:
         return torch.empty((b, heads, t, D), device="cuda").normal_(0.0, gain, generator=g).to(DTYPE)
 
     filters = torch.empty((M, D, WIDTH), device="cuda").normal_(0.0, (D * WIDTH) ** -0.5, generator=g).to(DTYPE)
-    r = Requests(n)
+    r = Requests(n, rows_each=rows_each)
     # prompts of odd lengths, one after the other; their memories into pages, all in one plan and one store
     memories = [compress(rows(KV, 1, t, D ** -0.5), rows(KV, 1, t, D ** -0.5), rows(HEADS, 1, t, D ** -0.5), filters)
                 for t in (100 + (i * 397) % 2500 for i in range(n))]
@@ -83,6 +89,7 @@ def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None) -> dict:
 
     one = torch.ones(n, dtype=torch.int32, device="cuda")
     ws, o = r.workspace(n, 1), torch.empty((n, HEADS, 1, D), dtype=DTYPE, device="cuda")
+    prompts = r.sums.clone()
     torch.cuda.synchronize()
     began = time.perf_counter()
     for _ in range(turns):                              # a token each; [n, heads, 1, d] as a decoding batch has them
@@ -94,6 +101,7 @@ def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None) -> dict:
             on_turn("token", r, q, k, v, o)
     torch.cuda.synchronize()
     seconds = time.perf_counter() - began
+    served = int((r.sums - prompts)[0])                 # tokens of requests that were not refused
 
     # request 0 ends, request 1 gets the user's next message, the others a token
     message = 77
@@ -108,8 +116,8 @@ def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None) -> dict:
     if on_turn:
         on_turn("message", r, q, k, v, o)
     torch.cuda.synchronize()
-    return {"tokens_per_s": n * turns / seconds, "us_per_turn": seconds / turns * 1e6, "memory_rows": sum(live),
-            "pages_given_back": int(r.totals[2]), "held": r.held.tolist(),
+    return {"tokens_per_s": served / seconds, "tokens": served, "refused": int(r.sums[3]), "us_per_turn": seconds / turns * 1e6,
+            "memory_rows": sum(live), "pages_given_back": int(r.totals[2]), "held": r.held.tolist(),
             "bytes_a_row": 2 * KV * (D // 2 + D // 32), "bytes_a_row_bf16": 2 * KV * D * 2}
 
 

@@ -440,7 +440,9 @@ typedef struct lococo_pages {
  *     `tables` (table_pages entries); row x of it, at position held[i] + x, gets its slot and its position written;
  *   - a request whose rows pass `tokens`, whose pages pass table_pages, or whose pages together with those all requests before
  *     it asked for are more than the ring had at the start of the call, is refused as a whole: it takes no page, held_after is
- *     held, the slots and positions of its rows are -1 (its place in the call stays);
+ *     held, the slots and positions of its rows are -1.  Its place in the call stays, so that an attention over this plan computes
+ *     rows of o for it, as if its queries stood at its last old rows: they have no meaning and are to be dropped where slots is -1
+ *     (totals[3] tells whether there are any).  No other request's rows depend on it;
  *   - a request at its end gives its pages back behind the ring's last one, its held_after is 0.  Pages given back can be taken
  *     from the next call on.
  * Rows of the call behind the last request's get -1.  ring [n_pages] holds the free pages: the entries ends[0] .. ends[1] - 1,

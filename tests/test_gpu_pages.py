@@ -332,6 +332,37 @@ def test_attention_views_scale_and_rows_of_nobody(dtype, d):
     check_attn(pages, q, tables, starts, held, run_attn(pages, q, tables, starts, held), scale=0.375)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128, 96])
+@pytest.mark.parametrize("asked", [1, 9, 40])
+def test_refused_requests_disturb_nobody(dtype, d, asked):
+    """Plan, store and attention of a turn in which one request is refused: its rows have no slots, its pages stay as they are, and the
+    other requests' rows are what they are without it."""
+    lens = [(40, 3), (96, asked), (70, 2)]                             # (held ahead of the turn, new): request 1 fills its table's 6 pages
+    pages, _, tables, _, _ = make_batch(141, dtype, 2, 2, d, 16, [(h + w, w) for h, w in lens])
+    held, tables = torch.tensor([h for h, _ in lens], **I32), tables[:, :6].contiguous()
+    own = [int(p) for row, h in zip(tables, held.tolist()) for p in row[:-(-h // 16)]]
+    free = [p for p in range(pages.c.n_pages) if p not in own]
+    ring, ends = torch.tensor(free + [-1] * (pages.c.n_pages - len(free)), **I32), torch.tensor([0, len(free)], device="cuda")
+    new, t, n = torch.tensor([w for _, w in lens], **I32), tables.cuda(), sum(w for _, w in lens)
+    after, ends2, starts, slots, at, totals = (torch.zeros(m, dtype=k, device="cuda") for m, k in (
+        (3, torch.int32), (2, torch.int64), (4, torch.int32), (n, torch.int32), (n, torch.int32), (4, torch.int32)))
+    lb.lococo_pages_plan(pages, new, held, t, ring, ends, after, ends2, starts, slots, at, totals)
+    assert totals.tolist()[3] == 1 and after[1] == held[1] and (slots[3:3 + asked] == -1).all() and (slots[:3] >= 0).all() and (slots[-2:] >= 0).all()
+    g = torch.Generator().manual_seed(9)
+    q, k, v = (torch.randn(1, h, n, d, generator=g).to(dtype).cuda() for h in (4, 2, 2))
+    mine = t[1, :-(-int(held[1]) // 16)].long()
+    before = [x[mine].clone() for x in (pages.k_codes, pages.k_scales, pages.v_codes, pages.v_scales)]
+    lb.lococo_pages_store(pages, k, v, slots)
+    for x, y in zip(before, (pages.k_codes, pages.k_scales, pages.v_codes, pages.v_scales)):
+        assert torch.equal(x, y[mine])
+    o = run_attn(pages, q, t.cpu(), starts.cpu(), after.cpu())
+    keep = [x for x in range(n) if not 3 <= x < 3 + asked]
+    others = run_attn(pages, q[:, :, keep].contiguous(), t.cpu()[[0, 2]], torch.tensor([0, 3, 5], dtype=torch.int32), after.cpu()[[0, 2]])
+    check_attn(pages, q[:, :, keep], t.cpu()[[0, 2]], torch.tensor([0, 3, 5], dtype=torch.int32), after.cpu()[[0, 2]], others)
+    check_attn(pages, q[:, :, keep], t.cpu()[[0, 2]], torch.tensor([0, 3, 5], dtype=torch.int32), after.cpu()[[0, 2]], o[:, :, keep])
+
+
 def test_attention_repeats_bit_for_bit():
     batch = make_batch(61, torch.bfloat16, 2, 4, 128, 64, [(5000, 1), (300, 1), (2222, 1)])
     first = run_attn(*batch)

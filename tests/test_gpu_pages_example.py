@@ -51,6 +51,29 @@ def test_example_serves_what_it_stored():
     assert got["held"][0] == 0 and got["held"][1] >= 77 and got["pages_given_back"] > 0
 
 
+def test_example_tells_and_drops_what_was_refused():
+    """Requests whose tables are full are refused turn after turn: counted, not among the tokens served, and zeros in their rows of o."""
+    ex = load_example()
+    seen = []
+
+    def on_turn(what, r, q, k, v, o):
+        at = r.slots.tolist()
+        starts, held = r.starts.tolist(), r.held.tolist()
+        gone = [i for i in range(r.n) if any(at[x] < 0 for x in range(starts[i], starts[i + 1]))]
+        for i in gone:
+            assert all(at[x] < 0 for x in range(starts[i], starts[i + 1]))      # as a whole
+            held[i] = 0                                                         # a plain request that holds nothing: zeros
+        seen.append((what, gone))
+        if gone or what == "message":
+            check_attn(r.pages, q, r.tables.cpu(), r.starts.cpu(), torch.tensor(held, dtype=torch.int32), o)
+
+    got = ex.serve(n=3, turns=66, rows_each=320, on_turn=on_turn)               # 256 slots of memory and 64 rows behind them
+    want = sum(len(gone) for _, gone in seen)
+    assert got["refused"] == want > 0 and seen[0][1] == [] and seen[-2][1] != [] and seen[-1][0] == "message"
+    assert got["tokens"] == 3 * 66 - sum(len(gone) for what, gone in seen if what == "token")
+    assert max(got["held"]) <= 320
+
+
 def test_turn_in_a_graph():
     """Plan, store and attention of a turn, captured once and replayed with other lengths, rows and queries in the same arrays."""
     pages, q, tables, starts, held = make_batch(7, torch.bfloat16, 2, 4, 128, 16, [(700, 1), (30, 1), (1500, 1), (1, 1)])
