@@ -534,3 +534,33 @@ def test_attention_leaves_rows_ahead_of_the_first_request(dtype, group, d, lens)
                          held.cuda(), most, int(held.max()), ws)
     assert (o[:, :, :ahead] == 3).all()
     check_attn(pages, q, tables, starts, held, o[:, :, ahead:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(3000, 1), (1700, 1)], [(2900, 7), (1000, 2)], [(3000, 40), (1800, 33)]])
+def test_attention_in_parts_keeps_nan_and_leaves_out_pages(dtype, d, lens):
+    """Marked blocks, and entries that are no page, where the rows of a request are shared out between workgroups and joined."""
+    pages, q, tables, starts, held = make_batch(131, dtype, 2, 2, d, 16, lens)
+    assert lb.lococo_pages_workspace_bytes(pages, len(lens), q.shape[2], max(w for _, w in lens), int(held.max())) > 0    # there are parts
+    place = lambda i, r: (int(tables[i, r // 16]), r % 16)
+    h, w = lens[0]
+    p, r = place(0, h - 1)
+    pages.v_scales[p, 1, 1, r] = 255                                   # the last row: request 0's last query only
+    p, r = place(0, h // 3)
+    pages.v_scales[p, 0, 0, r] = 255                                   # in the middle, one head's first 32 columns: all of its queries
+    h, w = lens[1]
+    p, r = place(1, h - 1 - w // 2)
+    pages.k_scales[p, 0, 1, r] = 255                                   # the second half of request 1's queries
+    for i, entries in ((0, (0, 5, 60, 61, 62, 63, 64, 90)), (1, (17, 40))):
+        for e in entries:
+            tables[i, e] = (-1, 10 ** 6, 2 ** 31 - 1, -(2 ** 31))[e % 4]
+    batch = (pages, q, tables, starts, held)
+    got = run_attn(*batch)
+    assert torch.isnan(got).any() and not torch.isnan(got).all()
+    check_attn(*batch, got)
+    tables[0, :] = -1                                                  # nothing of request 0 is there: zeros, joined from its parts
+    batch = (pages, q, tables, starts, held)
+    got = run_attn(*batch)
+    assert not got[:, :, :lens[0][1]].any()
+    check_attn(*batch, got)
