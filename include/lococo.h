@@ -470,10 +470,12 @@ LOCOCO_API lococo_status lococo_pages_load(const lococo_pages* pages, const int3
 /* The requests of an attention call, as lococo_pages_plan leaves them. */
 typedef struct lococo_requests {
   int32_t n;              /* requests, 1 .. 4096                                                             */
-  int32_t tokens;         /* rows of q and o                                                                 */
+  int32_t tokens;         /* rows of q and o; more than a launch takes, 2^24 workgroups, is LOCOCO_EUNSUPPORTED */
   int32_t table_pages;    /* entries of a table; table_pages * page_rows < 2^30                              */
-  int32_t max_new;        /* no request has more new rows, of those it is the caller's promise: what is over
-                             is left unwritten                                                               */
+  int32_t max_new;        /* no request has more new rows, by the caller's promise: of one that has, the rows
+                             of o are right or left unwritten, other requests' are right.  max_new * n is at
+                             least `tokens`, rows of nobody among them (LOCOCO_EINVAL): a call of 40 rows for
+                             32 requests with a token each says 2                                            */
   int32_t max_held;       /* about the most rows a request holds: how the work is dealt out, and with it the
                              order of fp32 sums, goes by it, nothing else                                    */
   const int32_t* tables;  /* device [n][table_pages]                                                         */

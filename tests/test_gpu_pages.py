@@ -564,3 +564,36 @@ def test_attention_in_parts_keeps_nan_and_leaves_out_pages(dtype, d, lens):
     got = run_attn(*batch)
     assert not got[:, :, :lens[0][1]].any()
     check_attn(*batch, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,d", [(4, 128), (20, 64), (2, 96)])
+@pytest.mark.parametrize("held", [60, 1500])
+def test_attention_of_a_padded_batch(dtype, group, d, held):
+    """A token each of five requests in arrays of eight rows: max_new 2 covers them, the last three are nobody's."""
+    lens = [(held, 1), (7, 1), (held // 2, 1), (64, 1), (1, 1)]
+    pages, q, tables, starts, rows = make_batch(151, dtype, 1, group, d, 16, lens)
+    wide = torch.cat((q, q[:, :, :3]), 2).cuda()
+    o = torch.full_like(wide, 3.0)
+    ws = lb.pages_workspace(pages, 5, 8, 2, held)
+    lb.lococo_pages_attn(pages, wide, o, tables.cuda(), starts.cuda(), rows.cuda(), 2, held, ws)
+    check_attn(pages, q, tables, starts, rows, o[:, :, :5].contiguous())
+    assert (o[:, :, 5:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,d", [(2, 64), (4, 128), (16, 64), (2, 96)])
+@pytest.mark.parametrize("lens", [[(60, 1), (90, 9), (33, 2), (5, 0)], [(2500, 1), (1800, 21), (900, 3), (10, 1)]])
+def test_attention_of_more_rows_than_promised(dtype, group, d, lens):
+    """A request with more new rows than max_new: its rows are right or as they were, all others right."""
+    pages, q, tables, starts, held = make_batch(161, dtype, 1, group, d, 16, lens)
+    want = run_attn(pages, q, tables, starts, held)
+    check_attn(pages, q, tables, starts, held, want)
+    tokens, most = q.shape[2], -(-q.shape[2] // len(lens))
+    assert most < lens[1][1] and all(w <= most for w in (lens[0][1], lens[2][1], lens[3][1]))
+    o = torch.full_like(q, 77.0, device="cuda")
+    ws = lb.pages_workspace(pages, len(lens), tokens, most, int(held.max()))
+    lb.lococo_pages_attn(pages, q.cuda(), o, tables.cuda(), starts.cuda(), held.cuda(), most, int(held.max()), ws)
+    a, b = starts.tolist()[1:3]
+    o[:, :, a:b] = torch.where(o[:, :, a:b] == 77, want[:, :, a:b], o[:, :, a:b])
+    check_attn(pages, q, tables, starts, held, o)

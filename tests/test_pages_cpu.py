@@ -62,6 +62,15 @@ def test_requests_are_checked(over, want):
     assert L.lococo_pages_attn(C.byref(p), C.byref(r), C.byref(t), C.byref(tensor(FAKE[9])), 3, None, 0, None) == want
 
 
+@pytest.mark.parametrize("n,tokens,least", [(32, 32, 1), (32, 40, 2), (32, 64, 2), (32, 65, 3), (1, 77, 77)])
+def test_max_new_covers_every_row_of_a_call(n, tokens, least):
+    """Rows that no request has count among those max_new * n has to cover."""
+    L, p, out = lb.lib(), pages(), C.c_size_t(0)
+    size = lambda most: L.lococo_pages_workspace_bytes(C.byref(p), C.byref(requests(n=n, tokens=tokens, max_new=most)), C.byref(out))
+    assert size(least) == lb.LOCOCO_OK and size(least - 1) == lb.LOCOCO_EINVAL
+    assert size(least - 1) == lb.LOCOCO_EINVAL and b"max_new" in L.lococo_last_error()
+
+
 def test_call_arguments_are_checked():
     L, p, t, u, out = lb.lib(), pages(), tensor(), tensor(FAKE[9]), C.c_size_t(0)
     ok = dict(tables=FAKE[4], starts=FAKE[5], held=FAKE[6])
