@@ -446,6 +446,8 @@ def lococo_pages_attn(pages: Pages, q, o, tables, starts, held, max_new: int, ma
     b, _, t, _ = q.shape
     if q.shape != o.shape or starts.numel() != n + 1 or held.numel() != n:
         raise ValueError("o, starts or held do not fit q and the tables")
+    if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError(f"expected a contiguous workspace on the device, got {workspace.device}, strides {workspace.stride()}")
     r = lococo_requests(n, b * t, width, max_new, max_held, *_numbers(_I32, tables, starts, held))
     ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().lococo_pages_attn(pages.ref, C.byref(r), C.byref(x), C.byref(y), max(t, 1), ws, ws_bytes, _stream_now()))

@@ -597,3 +597,15 @@ def test_attention_of_more_rows_than_promised(dtype, group, d, lens):
     a, b = starts.tolist()[1:3]
     o[:, :, a:b] = torch.where(o[:, :, a:b] == 77, want[:, :, a:b], o[:, :, a:b])
     check_attn(pages, q, tables, starts, held, o)
+
+
+def test_workspaces_of_the_host_are_refused():
+    """Nothing is launched with a workspace that the device cannot write, or that has gaps."""
+    pages, q, tables, starts, held = make_batch(171, torch.bfloat16, 1, 2, 64, 16, [(3000, 1)])
+    q, o = q.cuda(), torch.full_like(q, 5.0, device="cuda")
+    need = lb.lococo_pages_workspace_bytes(pages, 1, 1, 1, 3000)
+    assert need > 0
+    for ws in (torch.empty(need, dtype=torch.uint8), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(TypeError, match="workspace"):
+            lb.lococo_pages_attn(pages, q, o, tables.cuda(), starts.cuda(), held.cuda(), 1, 3000, ws)
+    assert (o == 5).all()
