@@ -56,7 +56,11 @@ class Requests:
     def attend(self, q, o, max_new: int, workspace):
         """Attention of the planned rows; zeros for those of refused requests, whose attention has no meaning."""
         lb.lococo_pages_attn(self.pages, q, o, self.tables, self.starts, self.held, max_new, self.longest, workspace)
-        o.masked_fill_((self.slots < 0).view(q.shape[0], 1, q.shape[2], 1), 0)
+        self.drop(o, self.slots)
+
+    @staticmethod
+    def drop(o, slots):
+        o.masked_fill_((slots < 0).view(o.shape[0], 1, o.shape[2], 1), 0)
 
     def workspace(self, tokens: int, max_new: int):
         return lb.pages_workspace(self.pages, self.n, tokens, max_new, self.most)
@@ -88,7 +92,8 @@ def serve(n: int = 32, turns: int = 64, seed: int = 0, on_turn=None, rows_each: 
     lb.lococo_pages_store(r.pages, torch.cat([m[0][:, :, :m[2]] for m in memories], 2), torch.cat([m[1][:, :, :m[2]] for m in memories], 2), slots)
 
     one = torch.ones(n, dtype=torch.int32, device="cuda")
-    ws, o = r.workspace(n, 1), torch.empty((n, HEADS, 1, D), dtype=DTYPE, device="cuda")
+    ws, o = r.workspace(n, 1), torch.zeros((n, HEADS, 1, D), dtype=DTYPE, device="cuda")
+    r.drop(o, slots[:n])                                # (a first call loads torch's kernels)
     prompts = r.sums.clone()
     torch.cuda.synchronize()
     began = time.perf_counter()
