@@ -408,10 +408,11 @@ LOCOCO_API lococo_status lococo_sequence_backward(const lococo_config* cfg, cons
  *
  * Format.  32 consecutive values of a row share a scale byte e, which stands for 2^(e - 127); a value is a sign and one of the
  * eight magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6 times that scale (codes 0 .. 7, + 8 for the sign).  Storing takes, for the largest
- * magnitude a of the 32, 2^E with E = floor(log2 a) - 2, one more if a exceeds 7/4 of its power of two, -100 at least and 125 at most, and the
- * code nearest to value / 2^E, ties to the even code.  32 values that hold an infinity or a NaN get the byte 255 and stand for
- * NaN all of them.  Reading gives exactly scale times magnitude in either storage type (magnitudes of scale bytes below 2 apart,
- * which storing never writes).
+ * magnitude a of the 32, 2^E with E = floor(log2 a) - 2, one more if a exceeds 7/4 of its power of two, -100 at least and 125
+ * at most, and the code nearest to value / 2^E, ties to the even code.  32 values that hold an infinity or a NaN get the byte
+ * 255 and stand for NaN all of them.  Reading gives exactly scale times magnitude in either storage type (scale bytes below 2
+ * and above 252, whose magnitudes may leave the type's range, apart: storing never writes them, and attention is not made for
+ * them).
  *   codes   [n_pages][n_kv_heads][page_rows][head_dim / 2] bytes, value 2i of a row in the low four bits of its byte i
  *   scales  [n_pages][n_kv_heads][head_dim / 32][page_rows] bytes
  * The slot of row r of page p is p * page_rows + r.  What slots that nobody holds contain is never read into a result.
@@ -461,7 +462,8 @@ LOCOCO_API lococo_status lococo_pages_plan(const lococo_pages* pages, int32_t n,
 
 /* Rows of k and v, [b, n_kv_heads, rows_per_batch, head_dim] views holding `tokens` rows (row i of the call is row
  * i % rows_per_batch of batch entry i / rows_per_batch), to 4 bits at slots[i]; a slot outside the pages (-1) leaves its row out.
- * Two rows of a call must not share a slot; a call of no rows does nothing.  lococo_pages_load is the way back: rows at slots outside the pages become zeros. */
+ * Two rows of a call must not share a slot; a call of no rows does nothing.  lococo_pages_load is the way back: rows at slots outside
+ * the pages become zeros. */
 LOCOCO_API lococo_status lococo_pages_store(const lococo_pages* pages, const lococo_tensor* k, const lococo_tensor* v,
                                             int32_t rows_per_batch, int32_t tokens, const int32_t* slots, void* stream);
 LOCOCO_API lococo_status lococo_pages_load(const lococo_pages* pages, const int32_t* slots, int32_t rows_per_batch,
@@ -483,15 +485,15 @@ typedef struct lococo_requests {
   const int32_t* held;    /* device [n]: rows held, the new ones among them (the plan's held_after)          */
 } lococo_requests;
 
-/* o = Attn(Q, K, V) of every request over its own rows: query x of a request with `new` queries stands at position
- * held - new + x and sees the rows up to and at its position (Eq. 1 with the cache in front, as in lococo_attn_only); a compressed
- * memory stored ahead of the tokens is thus seen by all of them.  A query that sees nothing (held below new) gets zeros, rows of o
- * that no request has are not written, rows whose table entry is no page are left out.  q and o: [b, n_q_heads, rows_per_batch,
- * head_dim] views of requests->tokens rows counted as in lococo_pages_store; o must not alias q.  Softmax and sums in fp32,
- * operands as stored; probabilities enter their product with 16 bits or more for LOCOCO_BF16, with all 24 for LOCOCO_F32.  A
- * visible row's NaN reaches the results of the queries that see it and no others.  Sums are divided at the end, by then over
- * exponentials of 1 at most: results are finite where the sum of a column's magnitudes over the visible rows is.  Identical calls return
- * the same bits.
+/* o = Attn(Q, K, V) of every request over its own rows: query x of a request with `new` queries stands at position held - new +
+ * x and sees the rows up to and at its position (Eq. 1 with the cache in front, as in lococo_attn_only); a compressed memory
+ * stored ahead of the tokens is thus seen by all of them.  A query that sees nothing (held below new, or scores of -infinity
+ * alone) gets zeros, rows of o that no request has are not written, rows whose table entry is no page are left out.  q and o:
+ * [b, n_q_heads, rows_per_batch, head_dim] views of requests->tokens rows counted as in lococo_pages_store; o must not alias q.
+ * Softmax and sums in fp32, operands as stored; probabilities enter their product with 16 bits or more for LOCOCO_BF16, with
+ * all 24 for LOCOCO_F32.  A visible row's NaN reaches the results of the queries that see it and no others.  Sums are divided
+ * at the end, by then over exponentials of 1 at most: results are finite where the sum of a column's magnitudes over the
+ * visible rows is.  Identical calls return the same bits.
  * head_dim 64 and 128 run on the matrix cores, others on vector arithmetic, a wave a row.
  * workspace: device, 256-byte aligned, lococo_pages_workspace_bytes of the same sizes, or of a larger max_held (may be 0). */
 LOCOCO_API lococo_status lococo_pages_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out);

@@ -14,10 +14,11 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;      //
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Plan.  Three running sums over the requests give every row's place: of the new rows (where a request's rows begin in the call), of
 // the pages needed (which of the free ones are whose) and of the pages given back.  Every workgroup computes them all, n numbers from
-// the L2, and places a share of the rows, one a lane where the device holds that many: no workgroup waits for another, and one launch does.  What this call writes no part of it reads:
-// a request's new table entries lie behind the ones it reads, what is given back goes to the ring behind its free part.
+// the L2, and places a share of the rows, one a lane where the device holds that many: no workgroup waits for another, and one launch
+// does.  What this call writes no part of it reads: a request's new table entries lie behind the ones it reads, what is given back goes
+// to the ring behind its free part.
 // Sums saturate at kPagesCap (addition cut off at a bound is associative for numbers >= 0): lengths that make no sense stay sums that
-// refuse.  Bound by the launch and some three round trips to memory: 5.5 us for 32 requests with a row each, 7.8 us for 512 with 52 K rows.
+// refuse.  Bound by the launch and some three round trips to memory: 5.3 us for 32 requests with a row each, 7.8 us for 512 with 52 K rows.
 constexpr int kPlanThreads = 256;
 
 __device__ __forceinline__ int32_t add_cap(int32_t a, int32_t b) { return min(a + b, kPagesCap); }
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
 // half a step of its own binade.  x 2^-E is exact and the conversion rounds to the nearest code, ties to even, so the codes follow from
 // the values alone.  Four lanes share a block, eight values each: every access is contiguous over a row; a lane takes a row's K and V, two
 // requests on their way instead of one (2048 rows of 32 heads there and back 22.4 us with a lane to either, 20.1 so).  Bound by memory: 42 MB
-// in 10.2 us stored, 9.2 us loaded (4.2 and 4.6 TB/s; a large copy 5.1).
+// in 10.5 us stored, 9.4 us loaded (4.0 and 4.5 TB/s; a large copy 5.1).
 constexpr int kRowThreads = 256;
 constexpr int32_t kMinExp = -100, kMaxExp = 125;     // of a scale: blocks of nothing but smaller values are zeros; 6 times it is finite
 

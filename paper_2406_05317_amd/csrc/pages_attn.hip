@@ -133,12 +133,13 @@ __global__ __launch_bounds__(kRowsThreads) void pages_attn_rows_k(PagesAttnArgs 
 // not leave fp32 by them.  Probabilities enter their product as the sum of two bf16 numbers (16 bits), for fp32
 // rows of three (all 24 bits), as their queries do.  One alone would save a third of the MFMAs (prompts of 2000 tokens 0.81 ms for 0.99 then),
 // but is off by as much as the rounding of a bf16 result wherever one key carries a column, be it by its probability or, as where new
-// rows stand beside the averages of a compressed memory, by the size of its value.  Their sum is taken of the same numbers, by a product
+// rows stand beside the averages of a compressed memory, by the size of its value.  Two are off by 2^-16 of the sum of |p v|: below a bf16
+// result's own rounding unless the values cancel to less than 2^-8 of that sum.  The row's sum is taken of the same numbers, by a product
 // with ones: no vector instruction adds.
 //
 // Bound, single tokens: by memory and by the start and end of a workgroup, some 7 us: 131072 keys of 8 heads, 143 MB, 27.6 us
 // (5.1 TB/s), and 4 for the join.  Many rows: by the instructions around 104 MFMAs a tile of 64 keys x 32 rows (vector port 68 % busy,
-// matrix pipe 44 %): 3349 tokens on up to 14 K keys of 32 heads 0.97 - 1.01 ms, 670 - 700 TFLOP/s of 4 d flops a pair.  Each wave asks
+// matrix pipe 44 %): 3349 tokens on up to 14 K keys of 32 heads 0.97 - 1.01 ms, 670 - 700 TFLOP/s (4 d flops a pair).  Each wave asks
 // for the codes of V a whole tile ahead; those of K for the next tile go into the registers the scores have just been taken from.
 constexpr int kTileWaves = 4, kTileKeys = 64;
 constexpr float kNoRef = -3.0e38f;             // below any score
@@ -427,10 +428,10 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void pages_attn_tile_k(TileArgs
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int t = 0; t < 4; ++t) e[4 * i + t] = __builtin_amdgcn_exp2f(fmaf(s[qb][t][2 * h + i], c, -ref[qb]));
-          bf16x8 part[PROBS];
-          split_parts<PROBS>(e, part);
+        bf16x8 part[PROBS];
+        split_parts<PROBS>(e, part);
 #pragma unroll
-          for (int k = 0; k < PROBS; ++k) p[qb][k][h] = part[k];
+        for (int k = 0; k < PROBS; ++k) p[qb][k][h] = part[k];
 #pragma unroll
         for (int k = PROBS - 1; k >= 0; --k) sum[qb] = mfma16(one, p[qb][k][h], sum[qb]);
       }
@@ -648,6 +649,8 @@ bool tile_fits(int d) { return d == 64 || d == 128; }
 //  - else as many as bring the launch to the workgroups that are resident at once, two a compute unit: more of them only add their
 //    starts and ends (a request of 131072 keys, 8 heads of 4: 37 us, with twice as many 42), unless requests differ in length: those of a
 //    batch of single tokens are cut half as long, so that short ones make room (32 requests of 128 .. 8192 keys: 27 us, without 36).
+// One number of parts holds for all requests, from the longest and from how many tiles there are.  So one that is far longer than the others
+// is cut into too few: 131072 keys, 8 kv heads of 4, take 33 us alone, 262 beside 31 single tokens on up to 8192 and 778 beside 63.
 constexpr int kPartTiles = 8;                  // a workspace holds parts of so many times the tiles that are resident: 68 MB at d = 128
 struct TilePlan { int tr, rows, splits, chunk, by_request; int64_t slots; size_t rows_all; };
 TilePlan tile_plan(int dtype, const PagesAttnArgs& a) {
