@@ -381,7 +381,7 @@ def _prepare_keep(c, g, rng):
         for mine, x in zip((s["pages"].k_codes, s["pages"].k_scales, s["pages"].v_codes, s["pages"].v_scales), arrays):
             mine.copy_(x)
         s["out"] = dict(held=torch.empty(n, **i32), ends=torch.empty(2, dtype=torch.int64, device="cuda"),
-                        sources=torch.empty(len(slots), **i32), targets=torch.empty(len(slots), **i32), totals=torch.empty(3, **i32))
+                        sources=torch.empty(len(slots), **i32), targets=torch.empty(len(slots), **i32), totals=torch.empty(2, **i32))
     else:
         s["arrays"] = [torch.cat((x, torch.zeros_like(x[:1]))) for x in arrays]
     return s
@@ -576,7 +576,7 @@ def _run_keep(s):
         scales[b // R, :, :, b % R] = scales[a // R, :, :, a % R]
     kc, ks, vc, vs = (x[:P] for x in (kc, ks, vc, vs))
     return dict(held=after.int(), ends=torch.stack((s["ends"][0], s["ends"][1] + give.sum())), sources=sources.int(), targets=targets.int(),
-                totals=torch.stack((on.sum(), moves.sum(), give.sum())).int(), ring=s["ring"], kc=kc, ks=ks, vc=vc, vs=vs)
+                totals=torch.stack((on.sum(), give.sum())).int(), ring=s["ring"], kc=kc, ks=ks, vc=vc, vs=vs)
 
 
 def _row_bytes(c):
@@ -757,5 +757,5 @@ def _exact_keep(s):
     i32 = dict(dtype=torch.int32, device="cuda")
     kc, ks, vc, vs = (torch.from_numpy(x).cuda() for x in arrays)
     return dict(held=torch.tensor(after, **i32), ends=torch.tensor([head, tail + len(back)], device="cuda"), sources=torch.tensor(sources, **i32),
-                targets=torch.tensor(targets, **i32), totals=torch.tensor([rows, sum(x >= 0 for x in sources), len(back)], **i32),
+                targets=torch.tensor(targets, **i32), totals=torch.tensor([rows, len(back)], **i32),
                 ring=torch.tensor(ring, **i32), kc=kc, ks=ks, vc=vc, vs=vs)
