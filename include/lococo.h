@@ -501,6 +501,115 @@ LOCOCO_API lococo_status lococo_pages_attn(const lococo_pages* pages, const loco
                                            const lococo_tensor* o, int32_t rows_per_batch, void* workspace, size_t ws_bytes,
                                            void* stream);
 
+/* ---- Norm and position rotation of query and key rows ------------------------------------------------------------------------
+ *
+ * What lies between a projection's rows and the q and k that the calls above take.  For every head of a row x of head_dim values:
+ *
+ *   n = x / sqrt(mean(x^2) + norm_eps) * w      (norm = 1; w = 1 without weights)      or n = x (norm = 0)
+ *   y_a = n_a cos(t) - n_b sin(t),  y_b = n_b cos(t) + n_a sin(t),  t = position * freqs[i]
+ *
+ * for the pairs i = 0 .. rotary_dim / 2 - 1 of channels (a, b); channels from rotary_dim on are n as it is.  Positions are whole
+ * numbers and t is their exact product with the fp32 frequency: its cosine and sine are right to fp32 at any position. */
+enum { LOCOCO_PAIRS_HALVES = 0,    /* pair i is the channels i and i + rotary_dim / 2 */
+       LOCOCO_PAIRS_ADJACENT = 1   /* pair i is the channels 2 i and 2 i + 1          */ };
+typedef struct lococo_rotation {
+  uint32_t struct_size;   /* sizeof(lococo_rotation)                                                      */
+  int32_t dtype;          /* LOCOCO_F32 / LOCOCO_BF16: type of the rows and of the weights                */
+  int32_t n_q_heads;      /* at most 65535 each                                                           */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* a multiple of 8, at most 256                                                 */
+  int32_t rotary_dim;     /* even, 0 (no rotation) .. head_dim                                            */
+  int32_t pairing;        /* LOCOCO_PAIRS_*                                                               */
+  int32_t norm;           /* 1: rows are divided by their root mean square; 0: they are not               */
+  float norm_eps;         /* 0 => 1e-6                                                                    */
+  const float* freqs;     /* device, rotary_dim / 2 frequencies in radians a position                     */
+  const void* q_weight;   /* device, head_dim weights a head, contiguous, or NULL; only with norm = 1     */
+  const void* k_weight;
+  int64_t q_weight_stride;/* elements between the weights of two heads; 0: all heads share the first's    */
+  int64_t k_weight_stride;
+} lococo_rotation;
+
+/* q_out, k_out = the above of q and k: [b, heads, rows_per_batch, head_dim] views of `tokens` rows counted as in
+ * lococo_pages_store.  positions: device [tokens], or NULL: a row's position is its number in its batch entry.  A row with a negative
+ * position is nobody's: its place in q_out and k_out is left as it is.  q and q_out may be NULL together, so may k and k_out.  q_out
+ * may be q and k_out k (the same strides then); else they must not overlap the inputs.  Arithmetic in fp32, one rounding at the end. */
+LOCOCO_API lococo_status lococo_rows_rotate(const lococo_rotation* rot, const lococo_tensor* q, const lococo_tensor* k,
+                                            const lococo_tensor* q_out, const lococo_tensor* k_out, int32_t rows_per_batch,
+                                            int32_t tokens, const int32_t* positions, void* stream);
+
+/* The way back, for training: q, k, positions as in the forward pass (the rows as they were before it).  Gradients are fp32 device
+ * arrays, contiguous, as those of lococo_sequence_backward are:
+ *     in   d_q_out [b, n_q_heads, rows_per_batch, head_dim], d_k_out [b, n_kv_heads, ...]: w.r.t. q_out, k_out
+ *     out  d_q, d_k, laid out the same: overwritten, rows of nobody with zeros; d_q may be d_q_out, d_k may be d_k_out
+ *     acc  d_q_weight, d_k_weight: ADDED to, [head_dim], or with a weight stride other than 0 as the weights lie; NULL: not wanted.
+ * Rounding of the forward pass's results is treated as the identity.  Identical calls return the same bits.
+ *   workspace: lococo_rows_rotate_backward_workspace_bytes bytes, 256-byte aligned; none without a weight's gradient. */
+LOCOCO_API lococo_status lococo_rows_rotate_backward_workspace_bytes(const lococo_rotation* rot, int32_t tokens, size_t* out);
+LOCOCO_API lococo_status lococo_rows_rotate_backward(const lococo_rotation* rot, const lococo_tensor* q, const lococo_tensor* k,
+                                                     int32_t rows_per_batch, int32_t tokens, const int32_t* positions,
+                                                     const float* d_q_out, const float* d_k_out, float* d_q, float* d_k,
+                                                     float* d_q_weight, float* d_k_weight, void* workspace, size_t ws_bytes,
+                                                     void* stream);
+
+/* A turn's new rows into the pages as a projection leaves them: q_out = q normed and turned, k normed and turned and v to 4 bits at
+ * slots[i]: lococo_rows_rotate and lococo_pages_store in one pass.  A slot outside the pages leaves its row of k and v out, a negative
+ * position its row of q_out as it is.  slots, positions: device [tokens], as lococo_pages_plan or lococo_pages_tree leaves them; two
+ * rows of a call must not share a slot.  Norm and rotation of k are in 64 bits: its codes are those nearest to the exact values, where
+ * lococo_pages_store would take those nearest to rounded ones.  rot and pages describe the same rows (type, heads, head_dim).  q_out may be q. */
+LOCOCO_API lococo_status lococo_pages_append(const lococo_pages* pages, const lococo_rotation* rot, const lococo_tensor* q,
+                                             const lococo_tensor* k, const lococo_tensor* v, const lococo_tensor* q_out,
+                                             int32_t rows_per_batch, int32_t tokens, const int32_t* slots, const int32_t* positions,
+                                             void* stream);
+
+/* ---- Trees of drafted tokens over paged rows ---------------------------------------------------------------------------------
+ *
+ * A turn in which a request brings several continuations at once, as a tree: its new rows are drafted tokens, each the child of an
+ * earlier one.  lococo_pages_plan gives them pages and slots as it does any new rows, and then
+ *
+ *   lococo_pages_tree       from the rows' parents: the position each stands at, and the mask of the new rows it sees
+ *   lococo_pages_append     the rows into their slots, turned by those positions
+ *   lococo_pages_attn_tree  attention under those masks
+ *   lococo_pages_keep       once it is known which rows are accepted: where they go, what a request holds then, pages given back
+ *   lococo_pages_move       (for every layer's pages) the kept rows to their places
+ *
+ * The next turn's plan takes held_after, ends_after and the ring of lococo_pages_keep.  Arrays of numbers are read when the kernels
+ * run, with the promises of the paged calls above.  n: requests, at most 4096; starts, held, slots, tables: as the plan leaves them. */
+
+/* parents [tokens]: of new row x of a request, the new row (0 .. x - 1, counted within the request) it continues, or -1: a root.
+ * Numbers that are no earlier row count as -1.  A row stands as many positions behind bases[i] as it has ancestors (bases NULL: behind
+ * held - new, so that a root's position is that of the request's first new row), and its mask holds its ancestors and itself: bit
+ * j % 32 of word j / 32 of the row's mask_words words (1 .. 8) is new row j.  Of a request with more than 32 * mask_words new rows
+ * those behind get position -1 and an empty mask, and so do rows that no request has.
+ *   out  masks [tokens][mask_words], positions [tokens] */
+LOCOCO_API lococo_status lococo_pages_tree(int32_t n, int32_t tokens, const int32_t* starts, const int32_t* held,
+                                           const int32_t* bases, const int32_t* parents, int32_t mask_words, uint32_t* masks,
+                                           int32_t* positions, void* stream);
+
+/* lococo_pages_attn with another rule of what a new row sees: all of its request's rows ahead of the new ones (positions 0 .. held -
+ * new - 1) and those new rows j, at position held - new + j, whose bit its mask has; any mask, not only a tree's.  A row's own bit
+ * counts like the others; a query that sees nothing gets zeros.  New rows that a mask has no bits for (mask_words is 1 .. 8) are not
+ * seen.  All else, the workspace (lococo_pages_workspace_bytes of the same sizes) and the promises on NaN among it, is as there. */
+LOCOCO_API lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
+                                                const lococo_tensor* o, int32_t rows_per_batch, const uint32_t* masks,
+                                                int32_t mask_words, void* workspace, size_t ws_bytes, void* stream);
+
+/* The new rows whose number in kept [tokens] is not 0 stay, in their order: the first of a request's takes the slot of its first new
+ * row, and so on.  slots: the plan's.  A request whose first new row has no slot was refused: it keeps what it held.
+ *   in      tables [n][table_pages], starts [n + 1], held [n] (the plan's held_after), slots, kept [tokens], ends [2] (ends_after)
+ *   in out  ring [n_pages]: pages that no row is left in go behind its last free one, request by request
+ *   out     held_after [n], ends_after [2], sources, targets [tokens]: the slots a kept row moves between, -1 for rows that do not
+ *           move; totals [2]: rows kept, pages given back.  Outputs are not inputs: a call can be repeated.
+ * Of `pages` page_rows and n_pages are used; the arrays may be NULL. */
+LOCOCO_API lococo_status lococo_pages_keep(const lococo_pages* pages, int32_t n, int32_t tokens, int32_t table_pages,
+                                           const int32_t* tables, const int32_t* starts, const int32_t* held, const int32_t* slots,
+                                           const int32_t* kept, int32_t* ring, const int64_t* ends, int32_t* held_after,
+                                           int64_t* ends_after, int32_t* sources, int32_t* targets, int32_t* totals, void* stream);
+
+/* The rows at sources to targets, codes and scales as they lie, K and V of every kv head.  starts, sources, targets: those of
+ * lococo_pages_keep (a row takes the place of an earlier one of its request, or stays; slots outside the pages are left out). */
+LOCOCO_API lococo_status lococo_pages_move(const lococo_pages* pages, int32_t n, int32_t tokens, const int32_t* starts,
+                                           const int32_t* sources, const int32_t* targets, void* stream);
+
 /* Optional per-kernel timing.  Between lococo_timing_begin() and
  * lococo_timing_end() every kernel the library launches (from any thread) is
  * bracketed by a pair of HIP events recorded on the stream it is launched on.

@@ -19,6 +19,7 @@ LOCOCO_OK, LOCOCO_EINVAL, LOCOCO_EUNSUPPORTED, LOCOCO_ESTATE, LOCOCO_EHIP, LOCOC
 LOCOCO_F32, LOCOCO_BF16 = 0, 1
 LOCOCO_IMPL_AUTO, LOCOCO_IMPL_GENERIC, LOCOCO_IMPL_MFMA = 0, 1, 2
 LOCOCO_FLAG_FILTERS_PREPARED = 1
+LOCOCO_PAIRS_HALVES, LOCOCO_PAIRS_ADJACENT = 0, 1
 (LOCOCO_OPT_RESET, LOCOCO_OPT_SPIN_LIMIT, LOCOCO_OPT_SCAN_PER_STEP, LOCOCO_OPT_CHAIN_SYNC_DEVICE,
  LOCOCO_OPT_LOGITS_TILES, LOCOCO_OPT_MAX_RESIDENT, LOCOCO_OPT_UNFUSED_KV, LOCOCO_OPT_NO_STEP_PIPELINE) = range(8)
 
@@ -30,7 +31,9 @@ EXPORTS = ["lococo_plan", "lococo_workspace_bytes", "lococo_attn_only", "lococo_
            "lococo_segment_step_noalloc", "lococo_sequence_backward_workspace_bytes",
            "lococo_sequence_backward",
            "lococo_pages_plan", "lococo_pages_store", "lococo_pages_load", "lococo_pages_workspace_bytes",
-           "lococo_pages_attn"]
+           "lococo_pages_attn",
+           "lococo_rows_rotate", "lococo_rows_rotate_backward_workspace_bytes", "lococo_rows_rotate_backward", "lococo_pages_append",
+           "lococo_pages_tree", "lococo_pages_attn_tree", "lococo_pages_keep", "lococo_pages_move"]
 
 
 class lococo_config(C.Structure):
@@ -85,6 +88,13 @@ class lococo_requests(C.Structure):
                 ("max_held", C.c_int32), ("tables", C.c_void_p), ("starts", C.c_void_p), ("held", C.c_void_p)]
 
 
+class lococo_rotation(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("pairing", C.c_int32), ("norm", C.c_int32),
+                ("norm_eps", C.c_float), ("freqs", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("q_weight_stride", C.c_int64), ("k_weight_stride", C.c_int64)]
+
+
 class LococoError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"lococo status {status}: {message}")
@@ -133,6 +143,15 @@ def lib():
         L.lococo_pages_load.argtypes = [pgp, C.c_void_p, i32, i32, tp, tp, C.c_void_p]
         L.lococo_pages_workspace_bytes.argtypes = [pgp, rqp, C.POINTER(C.c_size_t)]
         L.lococo_pages_attn.argtypes = [pgp, rqp, tp, tp, i32, C.c_void_p, C.c_size_t, C.c_void_p]
+        rtp, vp = C.POINTER(lococo_rotation), C.c_void_p
+        L.lococo_rows_rotate.argtypes = [rtp, tp, tp, tp, tp, i32, i32, vp, vp]
+        L.lococo_rows_rotate_backward_workspace_bytes.argtypes = [rtp, i32, C.POINTER(C.c_size_t)]
+        L.lococo_rows_rotate_backward.argtypes = [rtp, tp, tp, i32, i32] + [vp] * 8 + [C.c_size_t, vp]
+        L.lococo_pages_append.argtypes = [pgp, rtp, tp, tp, tp, tp, i32, i32, vp, vp, vp]
+        L.lococo_pages_tree.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.lococo_pages_attn_tree.argtypes = [pgp, rqp, tp, tp, i32, vp, i32, vp, C.c_size_t, vp]
+        L.lococo_pages_keep.argtypes = [pgp, i32, i32, i32] + [vp] * 13
+        L.lococo_pages_move.argtypes = [pgp, i32, i32] + [vp] * 4
         L.lococo_timing_begin.argtypes = []
         L.lococo_timing_end.argtypes = [C.POINTER(lococo_kernel_time), C.POINTER(C.c_int32)]
         for n in EXPORTS[:6] + EXPORTS[8:]:
@@ -264,6 +283,32 @@ class Pages:
         """(ring, ends) with every page free, as lococo_pages_plan takes them."""
         return (torch.arange(self.c.n_pages, dtype=torch.int32, device=self.device),
                 torch.tensor([0, self.c.n_pages], dtype=torch.int64, device=self.device))
+
+
+class Rotation:
+    """Norm and position rotation of a layer's query and key rows (lococo_rotation in lococo.h): `freqs` fp32 [rotary_dim / 2] in radians
+    a position (None: no rotation), weights [head_dim] for all heads or [heads, head_dim], of the rows' type."""
+
+    def __init__(self, *, dtype: torch.dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, freqs: torch.Tensor | None = None,
+                 adjacent: bool = False, norm: bool = False, norm_eps: float = 0.0, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None):
+        self.dtype, self.freqs, self.weights = dtype, freqs, (q_weight, k_weight)
+        if freqs is not None and (freqs.dtype is not torch.float32 or not freqs.is_cuda or not freqs.is_contiguous() or freqs.dim() != 1):
+            raise TypeError(f"expected frequencies [rotary_dim / 2] in fp32 on the device, got {tuple(freqs.shape)} of {freqs.dtype}, {freqs.device}")
+        strides = []
+        for w, heads in ((q_weight, n_q_heads), (k_weight, n_kv_heads)):
+            if w is not None and (w.dtype is not dtype or not w.is_cuda or not w.is_contiguous() or
+                                  tuple(w.shape) not in ((head_dim,), (heads, head_dim))):
+                raise TypeError(f"expected contiguous weights [{head_dim}] or [{heads}, {head_dim}] of {dtype} on the device, got "
+                                f"{tuple(w.shape)} of {w.dtype}, {w.device}")
+            strides.append(head_dim if w is not None and w.dim() == 2 else 0)
+        self.device = next((t.device.index for t in (freqs, q_weight, k_weight) if t is not None), None)
+        if any(t is not None and t.device.index != self.device for t in (freqs, q_weight, k_weight)):
+            raise TypeError("frequencies and weights are on different devices")
+        self.c = lococo_rotation(C.sizeof(lococo_rotation), _dtype_code(dtype), n_q_heads, n_kv_heads, head_dim,
+                                 0 if freqs is None else 2 * freqs.numel(), LOCOCO_PAIRS_ADJACENT if adjacent else LOCOCO_PAIRS_HALVES,
+                                 int(norm), norm_eps, _ptr(freqs), _ptr(q_weight), _ptr(k_weight), *strides)
+        self.ref = C.byref(self.c)
 
 
 def lococo_version() -> str:
@@ -453,6 +498,150 @@ def lococo_pages_attn(pages: Pages, q, o, tables, starts, held, max_new: int, ma
     _check(lib().lococo_pages_attn(pages.ref, C.byref(r), C.byref(x), C.byref(y), max(t, 1), ws, ws_bytes, _stream_now()))
 
 
+# The calls below also see to it that what they are given is on the current device, whose current stream they run on.
+def _here(*tensors):
+    """Device arrays on the current device; returns their addresses (None for None)."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise TypeError(f"expected arrays on the current device, {dev}, got one on {t.device}")
+    return [None if t is None else t.data_ptr() for t in tensors]
+
+
+def _whole(dtype, *arrays):
+    """Addresses of contiguous arrays of whole numbers on the current device (None for None)."""
+    for t in arrays:
+        if t is not None and (t.dtype is not dtype or not t.is_contiguous()):
+            raise TypeError(f"expected a contiguous {dtype} array on the device, got {t.dtype}, {t.device}, strides {t.stride()}")
+    return _here(*arrays)
+
+
+def _rotated(rot: Rotation, t: torch.Tensor, heads: int) -> lococo_tensor:
+    """View of a [b, heads, t, d] tensor of the rotation's type on the current device."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not rot.dtype or len(shape) != 4 or shape[1] != heads or shape[3] != rot.c.head_dim or stride[3] != 1:
+        raise TypeError(f"expected [b, {heads}, t, {rot.c.head_dim}] of {rot.dtype} on the device with the last axis contiguous, got "
+                        f"{tuple(shape)} of {t.dtype}, {t.device}, strides {stride}")
+    return lococo_tensor(_here(t)[0], stride[0], stride[1], stride[2])
+
+
+def _rotation_here(rot: Rotation):
+    if rot.device is not None and rot.device != torch._C._cuda_getDevice():
+        raise TypeError(f"the rotation's frequencies and weights are on device {rot.device}, not on the current one")
+
+
+def _rotated_pair(rot: Rotation, q, k):
+    """(views of q and k by reference, batch entries, rows of one)"""
+    if q is None and k is None:
+        raise ValueError("neither q nor k is given")
+    if q is not None and k is not None and (q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]):
+        raise ValueError(f"q and k of {tuple(q.shape)} and {tuple(k.shape)} are not of the same tokens")
+    some = k if q is None else q
+    views = [None if x is None else C.byref(_rotated(rot, x, h)) for x, h in ((q, rot.c.n_q_heads), (k, rot.c.n_kv_heads))]
+    return views, some.shape[0], some.shape[2]
+
+
+def _positions_of(positions, tokens):
+    if positions is not None and positions.numel() != tokens:
+        raise ValueError(f"{positions.numel()} positions for {tokens} rows")
+    return _whole(_I32, positions)[0]
+
+
+def lococo_rows_rotate(rot: Rotation, q, k, q_out, k_out, positions=None):
+    """q, k [b, heads, t, d] normed and turned by their rows' positions (None: 0 .. t - 1) into q_out, k_out; either may be None."""
+    _rotation_here(rot)
+    (x, y), b, t = _rotated_pair(rot, q, k)
+    (xo, yo), bo, to = _rotated_pair(rot, q_out, k_out)
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (b, t) != (bo, to):
+        raise ValueError("q_out, k_out do not fit q, k")
+    _check(lib().lococo_rows_rotate(rot.ref, x, y, xo, yo, max(t, 1), b * t, _positions_of(positions, b * t), _stream_now()))
+
+
+def lococo_rows_rotate_backward_workspace_bytes(rot: Rotation, tokens: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().lococo_rows_rotate_backward_workspace_bytes(rot.ref, tokens, C.byref(out)))
+    return out.value
+
+
+def lococo_rows_rotate_backward(rot: Rotation, q, k, positions, d_q_out, d_k_out, d_q, d_k, d_q_weight=None, d_k_weight=None, workspace=None):
+    """Gradients of lococo_rows_rotate: fp32, contiguous; d_q, d_k overwritten (they may be d_q_out, d_k_out), the weights' added to."""
+    _rotation_here(rot)
+    (x, y), b, t = _rotated_pair(rot, q, k)
+    for rows, grads in ((q, (d_q_out, d_q)), (k, (d_k_out, d_k))):
+        for g in grads:
+            if (g is None) != (rows is None) or (g is not None and (g.dtype is not torch.float32 or not g.is_contiguous() or g.shape != rows.shape)):
+                raise TypeError("expected contiguous fp32 gradients of the shapes of q and k")
+    for w, g in zip(rot.weights, (d_q_weight, d_k_weight)):
+        if g is not None and (w is None or g.dtype is not torch.float32 or not g.is_contiguous() or g.shape != w.shape):
+            raise TypeError("expected contiguous fp32 gradients of the shapes of the weights")
+    if workspace is not None and not workspace.is_contiguous():
+        raise TypeError(f"expected a contiguous workspace, got strides {workspace.stride()}")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    *grads, ws = _here(d_q_out, d_k_out, d_q, d_k, d_q_weight, d_k_weight, workspace)
+    _check(lib().lococo_rows_rotate_backward(rot.ref, x, y, max(t, 1), b * t, _positions_of(positions, b * t), *grads, ws, ws_bytes, _stream_now()))
+
+
+def lococo_pages_append(pages: Pages, rot: Rotation, q, k, v, q_out, slots, positions):
+    """New rows as a projection leaves them: q [b, n_q_heads, t, d] normed and turned into q_out, k so and v as it is to 4 bits at `slots`."""
+    _rotation_here(rot)
+    Hq, Hkv = pages.c.n_q_heads, pages.c.n_kv_heads
+    views = [C.byref(_rows(pages, x, h)) for x, h in ((q, Hq), (k, Hkv), (v, Hkv), (q_out, Hq))]
+    b, _, t, _ = q.shape
+    if q_out.shape != q.shape or k.shape != v.shape or k.shape[0] != b or k.shape[2] != t or slots.numel() != b * t:
+        raise ValueError("q, k, v, q_out or slots do not fit each other")
+    _here(pages.k_codes, q, k, v, q_out)
+    _check(lib().lococo_pages_append(pages.ref, rot.ref, *views, max(t, 1), b * t, _whole(_I32, slots)[0], _positions_of(positions, b * t),
+                                     _stream_now()))
+
+
+def lococo_pages_tree(starts, held, parents, masks, positions, bases=None):
+    """masks [tokens, words] (int32, words of bits) and positions [tokens] of the requests' trees from their rows' parents [tokens]."""
+    n = held.numel()
+    if starts.numel() != n + 1 or (bases is not None and bases.numel() != n):
+        raise ValueError("starts or bases do not fit held")
+    if masks.dim() != 2 or not masks.shape[0] == parents.numel() == positions.numel():
+        raise ValueError("masks, parents and positions do not fit each other")
+    s, h, b, p, m, x = _whole(_I32, starts, held, bases, parents, masks, positions)
+    _check(lib().lococo_pages_tree(n, parents.numel(), s, h, b, p, masks.shape[1], m, x, _stream_now()))
+
+
+def lococo_pages_attn_tree(pages: Pages, q, o, tables, starts, held, masks, max_new: int, max_held: int, workspace=None):
+    """lococo_pages_attn with the new rows that a row sees named by its mask, masks [tokens, words] (int32, words of bits)."""
+    x, y = _rows(pages, q, pages.c.n_q_heads), _rows(pages, o, pages.c.n_q_heads)
+    n, width = tables.shape
+    b, _, t, _ = q.shape
+    if q.shape != o.shape or starts.numel() != n + 1 or held.numel() != n or masks.dim() != 2 or masks.shape[0] != b * t:
+        raise ValueError("o, starts, held or masks do not fit q and the tables")
+    if workspace is not None and not workspace.is_contiguous():
+        raise TypeError(f"expected a contiguous workspace on the device, got {workspace.device}, strides {workspace.stride()}")
+    ws = _here(workspace, pages.k_codes, q, o)[0]
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    *numbers, m = _whole(_I32, tables, starts, held, masks)
+    r = lococo_requests(n, b * t, width, max_new, max_held, *numbers)
+    _check(lib().lococo_pages_attn_tree(pages.ref, C.byref(r), C.byref(x), C.byref(y), max(t, 1), m, masks.shape[1], ws, ws_bytes, _stream_now()))
+
+
+def lococo_pages_keep(pages: Pages, tables, starts, held, slots, kept, ring, ends, held_after, ends_after, sources, targets, totals):
+    """What becomes of a turn's rows and pages once the rows that `kept` marks stay (all arrays on the device: int32, ends int64)."""
+    n, width = tables.shape
+    tokens = slots.numel()
+    if not (starts.numel() - 1 == held.numel() == held_after.numel() == n and kept.numel() == sources.numel() == targets.numel() == tokens and
+            ring.numel() == pages.c.n_pages and ends.numel() == ends_after.numel() == 2 and totals.numel() == 2):
+        raise ValueError("arrays of the kept rows do not fit each other")
+    t, s, h, sl, k, r, ha, so, ta, to = _whole(_I32, tables, starts, held, slots, kept, ring, held_after, sources, targets, totals)
+    e, ea = _whole(_I64, ends, ends_after)
+    _check(lib().lococo_pages_keep(pages.ref, n, tokens, width, t, s, h, sl, k, r, e, ha, ea, so, ta, to, _stream_now()))
+
+
+def lococo_pages_move(pages: Pages, starts, sources, targets):
+    """The rows at sources to targets, as lococo_pages_keep leaves them, in one layer's pages."""
+    if sources.numel() != targets.numel() or starts.numel() < 2:
+        raise ValueError("sources and targets do not fit each other")
+    _here(pages.k_codes)
+    s, a, b = _whole(_I32, starts, sources, targets)
+    _check(lib().lococo_pages_move(pages.ref, starts.numel() - 1, sources.numel(), s, a, b, _stream_now()))
+
+
 def lococo_scan_status(cfg, workspace) -> int:
     """Synchronises; 0 = fine, 1 = a chain wait inside the one-launch scan of the lococo_sequence_forward or
     lococo_sequence_backward call that had this workspace gave up: its results are invalid."""
@@ -505,6 +694,12 @@ def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: i
     """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes (max_held may be larger than theirs)."""
     need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
     return torch.empty(need, dtype=torch.uint8, device=pages.device) if need else None
+
+
+def rotate_workspace(rot: Rotation, tokens: int, device="cuda") -> torch.Tensor | None:
+    """Allocate (through torch) the workspace of lococo_rows_rotate_backward calls of `tokens` rows with gradients of weights."""
+    need = lococo_rows_rotate_backward_workspace_bytes(rot, tokens)
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
 
 def config_for(w, impl: int = 0, **over) -> lococo_config:

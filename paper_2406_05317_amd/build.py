@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "liblococo.so")
 
 SOURCES = ["api.cpp", "generic_kernels.hip", "scan_small.hip", "compress_mfma.hip", "compress_step.hip", "attn_mfma.hip", "attn_decode.hip",
            "bwd_attn_mfma.hip", "bwd_conv_mfma.hip",
-           "backward_generic.hip", "tiled_mfma.hip", "pages.hip", "pages_attn.hip", "peaks.hip"]
+           "backward_generic.hip", "tiled_mfma.hip", "pages.hip", "pages_attn.hip", "rows_rotate.hip", "pages_append.hip",
+           "pages_tree.hip", "pages_attn_tree.hip", "peaks.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -38,7 +39,8 @@ EXTRA = {"compress_mfma.hip": COMPRESS, "compress_step.hip": COMPRESS,
          "attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "bwd_attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "bwd_conv_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "pages_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "pages_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "pages_attn_tree.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:

@@ -12,6 +12,7 @@
 
 #include "lococo_internal.h"
 #include "pages.h"
+#include "rotate.h"
 
 using namespace lococo;
 
@@ -63,12 +64,15 @@ lococo_status hip_fail(hipError_t e, const char* what) {
 // ---- optional per-kernel timing with HIP events (lococo_timing_begin / _end)
 enum KernelId { K_ATTN_GENERIC, K_FILL, K_CONV_GENERIC, K_NORM_GENERIC, K_MIX_GENERIC,
                 K_REPACK, K_COMPRESS_MFMA, K_ATTN_MFMA, K_ATTN_DECODE, K_ATTN_COLSUM, K_CONV_MFMA, K_MIX_MFMA,
-                K_COMPRESS_SMALL, K_BWD_WALK, K_PAGES_PLAN, K_PAGES_STORE, K_PAGES_LOAD, K_PAGES_ATTN, K_COUNT };
+                K_COMPRESS_SMALL, K_BWD_WALK, K_PAGES_PLAN, K_PAGES_STORE, K_PAGES_LOAD, K_PAGES_ATTN,
+                K_ROWS_ROTATE, K_ROWS_ROTATE_BACKWARD, K_PAGES_APPEND, K_PAGES_TREE, K_PAGES_ATTN_TREE, K_PAGES_KEEP, K_PAGES_MOVE, K_COUNT };
 const char* const kKernelNames[K_COUNT] = {"attn_generic", "fill", "conv_logits_generic",
                                            "normalise_generic", "mix_generic", "repack_filters",
                                            "compress_mfma", "attn_mfma", "attn_decode", "attn_colsum",
                                            "conv_logits_mfma", "mix_mfma", "compress_small", "bwd_walk",
-                                           "pages_plan", "pages_store", "pages_load", "pages_attn"};
+                                           "pages_plan", "pages_store", "pages_load", "pages_attn",
+                                           "rows_rotate", "rows_rotate_backward", "pages_append", "pages_tree",
+                                           "pages_attn_tree", "pages_keep", "pages_move"};
 struct TimedLaunch { int id; hipEvent_t start, stop; };
 std::mutex g_timing_mu;
 bool g_timing_on = false;
@@ -1920,6 +1924,275 @@ lococo_status lococo_pages_attn(const lococo_pages* pages, const lococo_requests
                 workspace ? ws_bytes : (size_t)0);
   KTimer kt(K_PAGES_ATTN, (hipStream_t)stream);
   HIP_TRY(launch_pages_attn(pages->dtype, a, workspace, (hipStream_t)stream), "attention over pages launch");
+  return LOCOCO_OK;
+}
+
+}  // extern "C"
+
+// ---- norm and position rotation of rows, and turns of drafted trees
+namespace {
+
+lococo_status check_rotation(const lococo_rotation* r) {
+  if (!r) return fail(LOCOCO_EINVAL, "rotation is NULL");
+  if (r->struct_size != sizeof(lococo_rotation))
+    return fail(LOCOCO_EINVAL, "rotation.struct_size is %u, this library expects %zu", r->struct_size, sizeof(lococo_rotation));
+  if (r->dtype != LOCOCO_F32 && r->dtype != LOCOCO_BF16)
+    return fail(LOCOCO_EINVAL, "rotation.dtype %d is neither LOCOCO_F32 nor LOCOCO_BF16", r->dtype);
+  if (r->n_q_heads <= 0 || r->n_kv_heads <= 0 || r->head_dim <= 0) return fail(LOCOCO_EINVAL, "head counts and head_dim must be positive");
+  if (r->n_q_heads > 65535 || r->n_kv_heads > 65535) return fail(LOCOCO_EUNSUPPORTED, "more than 65535 heads");
+  if (r->head_dim % 8 || r->head_dim > kRotateMaxDim)
+    return fail(LOCOCO_EUNSUPPORTED, "head_dim %d is not a multiple of 8 up to %d", r->head_dim, kRotateMaxDim);
+  if (r->rotary_dim < 0 || r->rotary_dim > r->head_dim || r->rotary_dim % 2)
+    return fail(LOCOCO_EINVAL, "rotary_dim %d is not an even number up to head_dim", r->rotary_dim);
+  if (r->pairing != LOCOCO_PAIRS_HALVES && r->pairing != LOCOCO_PAIRS_ADJACENT) return fail(LOCOCO_EINVAL, "pairing must be one of LOCOCO_PAIRS_*");
+  if (r->norm != 0 && r->norm != 1) return fail(LOCOCO_EINVAL, "norm must be 0 or 1");
+  if (!r->norm && !r->rotary_dim) return fail(LOCOCO_EINVAL, "neither a norm nor a rotation is asked for");
+  if (!(r->norm_eps >= 0.f) || std::isinf(r->norm_eps)) return fail(LOCOCO_EINVAL, "norm_eps must be finite and >= 0");
+  if (r->rotary_dim && (!r->freqs || ((uintptr_t)r->freqs & 3))) return fail(LOCOCO_EINVAL, "freqs is NULL or not 4-byte aligned");
+  const void* w[2] = {r->q_weight, r->k_weight};
+  const int64_t ws[2] = {r->q_weight_stride, r->k_weight_stride};
+  for (int i = 0; i < 2; ++i) {
+    if (w[i] && !r->norm) return fail(LOCOCO_EINVAL, "weights without a norm");
+    if (ws[i] && (!w[i] || ws[i] < r->head_dim)) return fail(LOCOCO_EINVAL, "a weight stride without weights, or below head_dim");
+    if (r->dtype == LOCOCO_BF16 ? ((uintptr_t)w[i] & 15) || ws[i] % 8 : ((uintptr_t)w[i] & 3) != 0)
+      return fail(LOCOCO_EINVAL, "weights need 16-byte aligned pointers and strides that are multiples of 8 (bf16), or 4-byte aligned ones (fp32)");
+  }
+  return LOCOCO_OK;
+}
+
+RotateView rotate_view(const lococo_rotation* r, bool q, bool k) {
+  return RotateView{r->freqs, {r->q_weight, r->k_weight}, {r->q_weight_stride, r->k_weight_stride}, {q ? r->n_q_heads : 0, k ? r->n_kv_heads : 0},
+                    r->head_dim, r->rotary_dim, r->pairing == LOCOCO_PAIRS_ADJACENT, r->norm, r->norm_eps > 0.f ? r->norm_eps : 1e-6f};
+}
+
+lococo_status check_rotated(const lococo_rotation* r, const lococo_tensor* t, const char* name, int32_t rows_per_batch, int32_t tokens) {
+  lococo_pages p{};
+  p.dtype = r->dtype;
+  p.head_dim = r->head_dim;
+  return check_rows(&p, t, name, rows_per_batch, tokens);
+}
+
+// rows written where they were read lie the same way there
+lococo_status check_in_place(const lococo_tensor* in, const lococo_tensor* out, const char* name) {
+  if (in->p == out->p && (in->stride_b != out->stride_b || in->stride_h != out->stride_h || in->stride_t != out->stride_t))
+    return fail(LOCOCO_EINVAL, "%s is written in place with other strides", name);
+  return LOCOCO_OK;
+}
+
+lococo_status check_turn(int32_t n, int32_t tokens) {
+  if (n <= 0 || tokens < 0) return fail(LOCOCO_EINVAL, "n must be positive, tokens not negative");
+  if (n > kPagesMaxRequests) return fail(LOCOCO_EUNSUPPORTED, "more than %d requests", kPagesMaxRequests);
+  if (tokens >= kPagesCap) return fail(LOCOCO_EUNSUPPORTED, "tokens must be below 2^30 - 1");
+  return LOCOCO_OK;
+}
+
+lococo_status check_masks(const uint32_t* masks, int32_t mask_words) {
+  if (mask_words <= 0) return fail(LOCOCO_EINVAL, "mask_words must be positive");
+  if (mask_words > kPagesMaxTree / 32) return fail(LOCOCO_EUNSUPPORTED, "masks name %d new rows of a request at most", kPagesMaxTree);
+  if (!masks || ((uintptr_t)masks & 3)) return fail(LOCOCO_EINVAL, "masks is NULL or not 4-byte aligned");
+  return LOCOCO_OK;
+}
+
+// arrays of whole numbers: none NULL, all aligned; no output an input or another output
+lococo_status check_arrays(const char* what, std::initializer_list<const void*> in, std::initializer_list<const void*> out) {
+  for (auto* list : {&in, &out})
+    for (const void* p : *list) {
+      if (!p) return fail(LOCOCO_EINVAL, "an array of %s is NULL", what);
+      if ((uintptr_t)p & 3) return fail(LOCOCO_EINVAL, "arrays of %s must be 4-byte aligned", what);
+    }
+  for (const void* const* o = out.begin(); o != out.end(); ++o) {
+    for (const void* i : in)
+      if (*o == i) return fail(LOCOCO_EINVAL, "an output of %s aliases an input", what);
+    for (const void* const* x = out.begin(); x != o; ++x)
+      if (*o == *x) return fail(LOCOCO_EINVAL, "outputs of %s alias each other", what);
+  }
+  return LOCOCO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lococo_status lococo_rows_rotate(const lococo_rotation* rot, const lococo_tensor* q, const lococo_tensor* k, const lococo_tensor* q_out,
+                                 const lococo_tensor* k_out, int32_t rows_per_batch, int32_t tokens, const int32_t* positions, void* stream) {
+  lococo_status st;
+  if ((st = check_rotation(rot))) return st;
+  if (!q && !k) return fail(LOCOCO_EINVAL, "q and k are both NULL");
+  if (!q != !q_out || !k != !k_out) return fail(LOCOCO_EINVAL, "rows without a place to write them, or the reverse");
+  if ((q && ((st = check_rotated(rot, q, "q", rows_per_batch, tokens)) || (st = check_rotated(rot, q_out, "q_out", rows_per_batch, tokens)))) ||
+      (k && ((st = check_rotated(rot, k, "k", rows_per_batch, tokens)) || (st = check_rotated(rot, k_out, "k_out", rows_per_batch, tokens)))))
+    return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if ((q && (st = check_in_place(q, q_out, "q"))) || (k && (st = check_in_place(k, k_out, "k")))) return st;
+  if (q && k && (q_out->p == k_out->p || q_out->p == k->p || k_out->p == q->p)) return fail(LOCOCO_EINVAL, "q_out or k_out aliases rows that are not its own");
+  if ((uintptr_t)positions & 3) return fail(LOCOCO_EINVAL, "positions is not 4-byte aligned");
+  RotateArgs a{};
+  a.rv = rotate_view(rot, q, k);
+  if (!rows_rotate_fits(a.rv, tokens)) return fail(LOCOCO_EUNSUPPORTED, "more rows than one launch takes");
+  if (q) {
+    a.in[0] = rows_view(q, rows_per_batch);
+    a.out[0] = rows_view(q_out, rows_per_batch);
+  }
+  if (k) {
+    a.in[1] = rows_view(k, rows_per_batch);
+    a.out[1] = rows_view(k_out, rows_per_batch);
+  }
+  a.positions = positions;
+  a.tokens = tokens;
+  a.t = rows_per_batch;
+  KTimer kt(K_ROWS_ROTATE, (hipStream_t)stream);
+  HIP_TRY(launch_rows_rotate(rot->dtype, a, (hipStream_t)stream), "rotation of rows launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_rows_rotate_backward_workspace_bytes(const lococo_rotation* rot, int32_t tokens, size_t* out) {
+  lococo_status st;
+  if (!out) return fail(LOCOCO_EINVAL, "out is NULL");
+  if ((st = check_rotation(rot))) return st;
+  if (tokens < 0) return fail(LOCOCO_EINVAL, "tokens must not be negative");
+  if (tokens >= kPagesCap) return fail(LOCOCO_EUNSUPPORTED, "tokens must be below 2^30 - 1");
+  *out = rot->q_weight || rot->k_weight ? align_up(rows_rotate_workspace_bytes(rotate_view(rot, true, true), tokens), 256) : 0;
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_rows_rotate_backward(const lococo_rotation* rot, const lococo_tensor* q, const lococo_tensor* k, int32_t rows_per_batch,
+                                          int32_t tokens, const int32_t* positions, const float* d_q_out, const float* d_k_out, float* d_q,
+                                          float* d_k, float* d_q_weight, float* d_k_weight, void* workspace, size_t ws_bytes, void* stream) {
+  lococo_status st;
+  if ((st = check_rotation(rot))) return st;
+  if (!q && !k) return fail(LOCOCO_EINVAL, "q and k are both NULL");
+  if ((q && (st = check_rotated(rot, q, "q", rows_per_batch, tokens))) || (k && (st = check_rotated(rot, k, "k", rows_per_batch, tokens)))) return st;
+  if ((d_q_weight && (!q || !rot->q_weight)) || (d_k_weight && (!k || !rot->k_weight)))
+    return fail(LOCOCO_EINVAL, "a gradient of weights that there are none of");
+  if (tokens == 0) return LOCOCO_OK;
+  if ((q && (!d_q_out || !d_q)) || (k && (!d_k_out || !d_k))) return fail(LOCOCO_EINVAL, "a gradient of q or k is NULL");
+  if (((uintptr_t)positions | (uintptr_t)d_q_out | (uintptr_t)d_k_out | (uintptr_t)d_q | (uintptr_t)d_k | (uintptr_t)d_q_weight |
+       (uintptr_t)d_k_weight) & 3)
+    return fail(LOCOCO_EINVAL, "positions and gradients must be 4-byte aligned");
+  const void* in[] = {q ? q->p : nullptr, k ? k->p : nullptr, rot->q_weight, rot->k_weight, rot->freqs, positions};
+  const void* out[] = {q ? d_q : nullptr, k ? d_k : nullptr, d_q_weight, d_k_weight};
+  for (int i = 0; i < 4; ++i) {
+    for (const void* p : in)
+      if (out[i] && out[i] == p) return fail(LOCOCO_EINVAL, "a gradient aliases an input");
+    for (int j = 0; j < i; ++j)
+      if (out[i] && out[i] == out[j]) return fail(LOCOCO_EINVAL, "gradients alias each other");
+  }
+  if (q && k && (d_q == d_k_out || d_k == d_q_out)) return fail(LOCOCO_EINVAL, "d_q aliases d_k_out, or d_k d_q_out");
+  if ((d_q_weight && (d_q_weight == d_q_out || d_q_weight == d_k_out)) || (d_k_weight && (d_k_weight == d_q_out || d_k_weight == d_k_out)))
+    return fail(LOCOCO_EINVAL, "a weight's gradient aliases an upstream one");
+  RotateBackArgs a{};
+  a.rv = rotate_view(rot, q, k);
+  if (!rows_rotate_fits(a.rv, tokens)) return fail(LOCOCO_EUNSUPPORTED, "more rows than one launch takes");
+  const size_t need = d_q_weight || d_k_weight ? align_up(rows_rotate_workspace_bytes(rotate_view(rot, true, true), tokens), 256) : 0;
+  if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
+    return fail(LOCOCO_EWORKSPACE, "the weights' gradients need %zu bytes of workspace, 256-byte aligned (got %zu)", need, workspace ? ws_bytes : (size_t)0);
+  if (q) a.in[0] = rows_view(q, rows_per_batch);
+  if (k) a.in[1] = rows_view(k, rows_per_batch);
+  a.gy[0] = d_q_out;
+  a.gy[1] = d_k_out;
+  a.gx[0] = d_q;
+  a.gx[1] = d_k;
+  a.gw[0] = d_q_weight;
+  a.gw[1] = d_k_weight;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.t = rows_per_batch;
+  KTimer kt(K_ROWS_ROTATE_BACKWARD, (hipStream_t)stream);
+  HIP_TRY(launch_rows_rotate_backward(rot->dtype, a, workspace, (hipStream_t)stream), "rotation's way back launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_append(const lococo_pages* pages, const lococo_rotation* rot, const lococo_tensor* q, const lococo_tensor* k,
+                                  const lococo_tensor* v, const lococo_tensor* q_out, int32_t rows_per_batch, int32_t tokens,
+                                  const int32_t* slots, const int32_t* positions, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_rotation(rot))) return st;
+  if (rot->dtype != pages->dtype || rot->n_q_heads != pages->n_q_heads || rot->n_kv_heads != pages->n_kv_heads || rot->head_dim != pages->head_dim)
+    return fail(LOCOCO_EINVAL, "rotation and pages are of different rows");
+  if ((st = check_rows(pages, q, "q", rows_per_batch, tokens)) || (st = check_rows(pages, k, "k", rows_per_batch, tokens)) ||
+      (st = check_rows(pages, v, "v", rows_per_batch, tokens)) || (st = check_rows(pages, q_out, "q_out", rows_per_batch, tokens)))
+    return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if ((st = check_in_place(q, q_out, "q"))) return st;
+  if (q_out->p == k->p || q_out->p == v->p) return fail(LOCOCO_EINVAL, "q_out aliases k or v");
+  if (!slots || !positions || (((uintptr_t)slots | (uintptr_t)positions) & 3))
+    return fail(LOCOCO_EINVAL, "slots or positions is NULL or not 4-byte aligned");
+  const PagesView pg = pages_view(pages);
+  if (!pages_append_fits(pg, tokens)) return fail(LOCOCO_EUNSUPPORTED, "more rows than one launch takes");
+  KTimer kt(K_PAGES_APPEND, (hipStream_t)stream);
+  HIP_TRY(launch_pages_append(pages->dtype, pg, rotate_view(rot, true, true), rows_view(q, rows_per_batch), rows_view(k, rows_per_batch),
+                              rows_view(v, rows_per_batch), rows_view(q_out, rows_per_batch), tokens, slots, positions, (hipStream_t)stream),
+          "append to pages launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_tree(int32_t n, int32_t tokens, const int32_t* starts, const int32_t* held, const int32_t* bases,
+                                const int32_t* parents, int32_t mask_words, uint32_t* masks, int32_t* positions, void* stream) {
+  lococo_status st;
+  if ((st = check_turn(n, tokens))) return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if ((st = check_masks(masks, mask_words)) ||
+      (st = check_arrays("the trees", {starts, held, parents, bases ? bases : held}, {masks, positions})))
+    return st;
+  PagesTreeArgs a{n, tokens, mask_words, starts, held, bases, parents, masks, positions};
+  KTimer kt(K_PAGES_TREE, (hipStream_t)stream);
+  HIP_TRY(launch_pages_tree(a, (hipStream_t)stream), "trees launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
+                                     const lococo_tensor* o, int32_t rows_per_batch, const uint32_t* masks, int32_t mask_words,
+                                     void* workspace, size_t ws_bytes, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_requests(pages, requests, true)) ||
+      (st = check_rows(pages, q, "q", rows_per_batch, requests->tokens)) ||
+      (st = check_rows(pages, o, "o", rows_per_batch, requests->tokens)))
+    return st;
+  if (requests->tokens == 0) return LOCOCO_OK;
+  if (o->p == q->p) return fail(LOCOCO_EINVAL, "o aliases q");
+  if ((st = check_masks(masks, mask_words))) return st;
+  PagesAttnArgs a = pages_attn_args(pages, requests);
+  a.q = rows_view(q, rows_per_batch);
+  a.o = rows_view(o, rows_per_batch);
+  a.max_held = (int32_t)std::min<int64_t>(a.max_held, (int64_t)a.table_pages * pages->page_rows);
+  const size_t need = align_up(pages_attn_workspace_bytes(pages->dtype, a), 256);
+  if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
+    return fail(LOCOCO_EWORKSPACE, "attention over pages needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,
+                workspace ? ws_bytes : (size_t)0);
+  KTimer kt(K_PAGES_ATTN_TREE, (hipStream_t)stream);
+  HIP_TRY(launch_pages_attn_tree(pages->dtype, a, masks, mask_words, workspace, (hipStream_t)stream), "attention over pages launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_keep(const lococo_pages* pages, int32_t n, int32_t tokens, int32_t table_pages, const int32_t* tables,
+                                const int32_t* starts, const int32_t* held, const int32_t* slots, const int32_t* kept, int32_t* ring,
+                                const int64_t* ends, int32_t* held_after, int64_t* ends_after, int32_t* sources, int32_t* targets,
+                                int32_t* totals, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, false)) || (st = check_turn(n, tokens))) return st;
+  if (table_pages <= 0) return fail(LOCOCO_EINVAL, "table_pages must be positive");
+  if ((int64_t)table_pages * pages->page_rows >= kPagesCap) return fail(LOCOCO_EUNSUPPORTED, "table_pages * page_rows must be below 2^30 - 1");
+  if ((st = check_arrays("the kept rows", {tables, starts, held, ends}, {ring, held_after, ends_after, totals}))) return st;
+  if (tokens && (st = check_arrays("the kept rows", {tables, starts, held, slots, kept, ends}, {ring, held_after, ends_after, sources, targets, totals})))
+    return st;
+  if (((uintptr_t)ends | (uintptr_t)ends_after) & 7) return fail(LOCOCO_EINVAL, "ends and ends_after must be 8-byte aligned");
+  const PagesView v = pages_view(pages);
+  PagesKeepArgs a{n, tokens, table_pages, v.page_rows, v.page_shift, v.n_pages, starts, held, slots, kept, tables, ring, ends, held_after, ends_after,
+                  sources, targets, totals};
+  KTimer kt(K_PAGES_KEEP, (hipStream_t)stream);
+  HIP_TRY(launch_pages_keep(a, (hipStream_t)stream), "keeping rows launch");
+  return LOCOCO_OK;
+}
+
+lococo_status lococo_pages_move(const lococo_pages* pages, int32_t n, int32_t tokens, const int32_t* starts, const int32_t* sources,
+                                const int32_t* targets, void* stream) {
+  lococo_status st;
+  if ((st = check_pages(pages, true)) || (st = check_turn(n, tokens))) return st;
+  if (tokens == 0) return LOCOCO_OK;
+  if ((st = check_arrays("the moved rows", {starts, sources, targets}, {}))) return st;
+  PagesMoveArgs a{pages_view(pages), n, tokens, starts, sources, targets};
+  KTimer kt(K_PAGES_MOVE, (hipStream_t)stream);
+  HIP_TRY(launch_pages_move(a, (hipStream_t)stream), "moving rows launch");
   return LOCOCO_OK;
 }
 

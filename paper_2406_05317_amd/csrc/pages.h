@@ -53,10 +53,47 @@ struct PagesAttnArgs {
   const int32_t* held;
 };
 
+// positions and masks of a turn's trees
+struct PagesTreeArgs {
+  int32_t n, tokens, words;
+  const int32_t* starts;
+  const int32_t* held;
+  const int32_t* bases;                        // null: held less the new rows
+  const int32_t* parents;
+  uint32_t* masks;
+  int32_t* positions;
+};
+
+// what becomes of a turn's rows and pages once some of the rows are kept
+struct PagesKeepArgs {
+  int32_t n, tokens, table_pages, page_rows, page_shift, n_pages;
+  const int32_t* starts;
+  const int32_t* held;
+  const int32_t* slots;
+  const int32_t* kept;
+  const int32_t* tables;
+  int32_t* ring;
+  const int64_t* ends;
+  int32_t* held_after;
+  int64_t* ends_after;
+  int32_t* sources;
+  int32_t* targets;
+  int32_t* totals;
+};
+
+struct PagesMoveArgs {
+  PagesView pg;
+  int32_t n, tokens;
+  const int32_t* starts;
+  const int32_t* sources;
+  const int32_t* targets;
+};
+
 constexpr int kPagesMaxRequests = 4096;       // the plan's lists lie in LDS
 constexpr int kPagesMaxHeadDim = 256;
 constexpr int kPagesMinRows = 16, kPagesMaxRows = 1024;
 constexpr int32_t kPagesCap = 0x3fffffff;     // rows of a call, slots, rows of a request: below
+constexpr int kPagesMaxTree = 256;            // new rows of a request that masks can name, a multiple of 32
 
 // ---- pages.hip
 hipError_t launch_pages_plan(const PagesPlanArgs& a, hipStream_t s);
@@ -65,9 +102,15 @@ hipError_t launch_pages_store(int dtype, const PagesView& pg, const RowsView& k,
                               const int32_t* slots, hipStream_t s);
 hipError_t launch_pages_load(int dtype, const PagesView& pg, const RowsView& k, const RowsView& v, int32_t tokens,
                              const int32_t* slots, hipStream_t s);
+// ---- pages_tree.hip
+hipError_t launch_pages_tree(const PagesTreeArgs& a, hipStream_t s);
+hipError_t launch_pages_keep(const PagesKeepArgs& a, hipStream_t s);
+hipError_t launch_pages_move(const PagesMoveArgs& a, hipStream_t s);
 // ---- pages_attn.hip
 bool pages_attn_fits(int dtype, const PagesAttnArgs& a);     // a launch takes the work
 size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a);
 hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace, hipStream_t s);
+// ---- pages_attn_tree.hip: the same sizes and workspace, a mask of `words` words for each of the call's rows
+hipError_t launch_pages_attn_tree(int dtype, const PagesAttnArgs& a, const uint32_t* masks, int32_t words, void* workspace, hipStream_t s);
 
 }  // namespace lococo

@@ -1,5 +1,6 @@
 // The plan of a turn over paged requests, and rows to 4 bits and back.
 #include "pages.h"
+#include "pages_codes.h"
 
 #include <type_traits>
 
@@ -170,14 +171,10 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Rows to 4 bits.  A block of 32 values has the scale 2^E, E = floor(log2 of the largest magnitude) - 2, one more where that magnitude
-// exceeds 1.75 times its power of two: then no value is more than 7 steps of the scale, and the largest code, 6, is off by no more than
-// half a step of its own binade.  x 2^-E is exact and the conversion rounds to the nearest code, ties to even, so the codes follow from
-// the values alone.  Four lanes share a block, eight values each: every access is contiguous over a row; a lane takes a row's K and V, two
+// Rows to 4 bits (pages_codes.h): every access is contiguous over a row; a lane takes a row's K and V, two
 // requests on their way instead of one (2048 rows of 32 heads there and back 22.4 us with a lane to either, 20.1 so).  Bound by memory: 42 MB
 // in 10.5 us stored, 9.4 us loaded (4.0 and 4.5 TB/s; a large copy 5.1).
 constexpr int kRowThreads = 256;
-constexpr int32_t kMinExp = -100, kMaxExp = 125;     // of a scale: blocks of nothing but smaller values are zeros; 6 times it is finite
 
 template <typename T>
 __device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
@@ -217,21 +214,8 @@ __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsV
   const int64_t at = (int64_t)page * pg.Hkv + head;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    uint32_t top = 0;                            // magnitudes as whole numbers: their order, with infinities and NaN on top
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[j][i]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const int32_t e = (int32_t)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
-    const uint32_t byte = top >= 0x7f800000u ? 255u : (uint32_t)(min(max(e, kMinExp), kMaxExp) + 127);
-    uint32_t code = 0;
-    if (byte != 255u) {
-      const float s = __uint_as_float(byte << 23);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][0], x[j][1], s, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][2], x[j][3], s, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][4], x[j][5], s, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[j][6], x[j][7], s, 3);
-    }
+    uint32_t byte;
+    const uint32_t code = four_bits(x[j], &byte);
     *(uint32_t*)((j ? pg.v_codes : pg.k_codes) + (at * pg.page_rows + row) * (pg.d / 2) + 4 * c) = code;
     if ((c & 3) == 0) (j ? pg.v_scales : pg.k_scales)[(at * (pg.d / 32) + c / 4) * pg.page_rows + row] = (uint8_t)byte;
   }
