@@ -3,9 +3,9 @@
 //   n = x / sqrt(mean(x^2) + eps) * w        (or n = x)
 //   y_a = n_a cos - n_b sin, y_b = n_b cos + n_a sin        (a, b) the two channels of pair i, the angle position * freqs[i]
 //
-// A row is P lanes of eight consecutive channels (P a power of two, lanes behind the row idle), so that a mean is a few exchanges inside a
-// wave and every access is 16 bytes or more.  What a lane's channels are turned against it loads once more, from where the lane beside it
-// has just had it fetched.  A workgroup's rows stand at few positions: their cosines and sines are computed once, to LDS, for all heads.
+// A row is P lanes of four pairs (P a power of two, lanes behind the row idle): both channels of a pair are a lane's own, a mean is a few
+// exchanges inside a wave.  A workgroup's rows stand at few positions: their cosines and sines are computed once, to LDS, for all heads, and a
+// lane keeps its four pairs' in registers from head to head, times the weights where all heads share them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -34,10 +34,16 @@ struct RotateShape {
   int32_t lp, lt;                              // P = 2^lp lanes to a row
   int32_t hb;                                  // heads of a workgroup
 };
+inline int32_t lanes_log(int32_t d) {
+  int32_t lp = 0;
+  while (8 << lp < d) ++lp;
+  return lp;
+}
 
 namespace rotate_detail {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t w4;
+typedef __attribute__((ext_vector_type(2))) uint32_t w2;
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f4_any;          // fp32 rows begin at any float
 
 template <typename T>
@@ -77,37 +83,96 @@ __device__ __forceinline__ const T* row_at(const RowsView& r, int32_t token, int
   return (const T*)r.p + b * r.sb + head * r.sh + t * r.st;
 }
 
-// Which channels a lane's, c0 .. c0 + 7, are turned against.
+template <typename T>
+__device__ __forceinline__ void read4(const T* p, float (&x)[4]) {
+  if constexpr (std::is_same<T, float>::value) {
+    const f4_any v = *(const f4_any*)p;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = v[k];
+  } else {
+    const w2 v = *(const w2*)p;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      x[2 * k] = __uint_as_float(v[k] << 16);
+      x[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void write4(T* p, const float (&x)[4]) {
+  if constexpr (std::is_same<T, float>::value) {
+    *(f4_any*)p = f4_any{x[0], x[1], x[2], x[3]};
+  } else {
+    __align__(8) __bf16 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (__bf16)x[i];
+    *(w2*)p = *(const w2*)y;
+  }
+}
+
+// The four pairs of a lane, q0 .. q0 + 3 of the row's d / 2; those from r / 2 on are not turned.
 enum PairKind {
-  kHalves8,                                    // channels j and j + r / 2, r / 2 a multiple of 8: a lane's are all first ones, all second ones
-  kHalves,                                     // or not turned at all; any other r
-  kAdjacent                                    // channels 2 j and 2 j + 1: pairs do not leave a lane
+  kHalves4,                                    // channels q and q + r / 2, r a multiple of 8; not turned: halves of the rest, likewise
+  kHalves,                                     // any other r; the rest two by two
+  kAdjacent                                    // channels 2 q and 2 q + 1
 };
 template <int KIND>
-struct Partners {
-  int32_t c0, half, r;
-  __device__ __forceinline__ int32_t pair(int i) const {
-    const int32_t c = c0 + i;
-    return KIND == kAdjacent ? c >> 1 : c < half ? c : c - half;
+struct Pairs {
+  int32_t q0, half, r, d;
+  __device__ __forceinline__ bool in() const { return 2 * q0 < d; }
+  __device__ __forceinline__ bool turned(int i) const { return q0 + (KIND == kHalves4 ? 0 : i) < half; }
+  __device__ __forceinline__ int32_t first(int i) const {
+    const int32_t q = q0 + i;
+    return KIND == kAdjacent ? 2 * q : q < half ? q : KIND == kHalves4 ? half + q : 2 * q;
   }
-  __device__ __forceinline__ bool turned(int i) const { return c0 + (KIND == kHalves8 ? 0 : i) < r; }
-  __device__ __forceinline__ bool second(int i) const { return KIND == kAdjacent ? i & 1 : c0 + (KIND == kHalves8 ? 0 : i) >= half; }
-  // the partners of the lane's channels in a row of a type, `own` those channels
+  __device__ __forceinline__ int32_t second(int i) const {
+    const int32_t q = q0 + i;
+    return KIND == kAdjacent ? 2 * q + 1 : q < half ? q + half : KIND == kHalves4 ? q + d / 2 : 2 * q + 1;
+  }
   template <typename T>
-  __device__ __forceinline__ void load(const T* row, const float (&own)[8], float (&x)[8]) const {
-    if constexpr (KIND == kAdjacent) {
+  __device__ __forceinline__ void load(const T* row, float (&a)[4], float (&b)[4]) const {
+    if constexpr (KIND == kHalves4) {
+      read4(row + first(0), a);
+      read4(row + second(0), b);
+    } else if constexpr (KIND == kAdjacent) {
+      float x[8];
+      read8(row + 2 * q0, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = own[i ^ 1];
-    } else if constexpr (KIND == kHalves8) {
-      if (c0 < r) read8(row + (c0 < half ? c0 + half : c0 - half), x);
+      for (int i = 0; i < 4; ++i) {
+        a[i] = x[2 * i];
+        b[i] = x[2 * i + 1];
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c0 + i < r) x[i] = (float)row[c0 + i < half ? c0 + i + half : c0 + i - half];
+      for (int i = 0; i < 4; ++i) {
+        a[i] = (float)row[first(i)];
+        b[i] = (float)row[second(i)];
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, const float (&a)[4], const float (&b)[4]) const {
+    if constexpr (KIND == kHalves4) {
+      write4(row + first(0), a);
+      write4(row + second(0), b);
+    } else if constexpr (KIND == kAdjacent) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = a[i];
+        x[2 * i + 1] = b[i];
+      }
+      write8(row + 2 * q0, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        row[first(i)] = (T)a[i];
+        row[second(i)] = (T)b[i];
+      }
     }
   }
 };
-inline PairKind pair_kind(int32_t r, int32_t adjacent) { return adjacent ? kAdjacent : r % 16 ? kHalves : kHalves8; }
+inline PairKind pair_kind(int32_t r, int32_t adjacent) { return adjacent ? kAdjacent : r % 8 ? kHalves : kHalves4; }
 
 // whole turns left out of the angle in 64 bits (position * frequency is exact there): half turns in [-1, 1]
 __device__ __forceinline__ float half_turns(int32_t position, float freq) {
@@ -115,12 +180,40 @@ __device__ __forceinline__ float half_turns(int32_t position, float freq) {
   return (float)(h - 2.0 * rint(h * 0.5));
 }
 
-// sums over the P lanes of a row
-template <typename R>
-__device__ __forceinline__ R row_sum(R x, int32_t lp) {
+// sums over the P lanes of a row; in fp32 up to 16 lanes without a trip through the LDS crossbar
+template <int CTRL>
+__device__ __forceinline__ float beside(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_sum(float x, int32_t lp) {
+  if (lp > 0) x += beside<0xb1>(x);            // lanes 1, 0, 3, 2 of four
+  if (lp > 1) x += beside<0x4e>(x);            // lanes 2, 3, 0, 1
+  if (lp > 2) x += beside<0x141>(x);           // eight, the other way round: the other four's sum
+  if (lp > 3) x += beside<0x140>(x);           // sixteen
+  if (lp > 4) x += __shfl_xor(x, 16);
+  return x;
+}
+__device__ __forceinline__ double row_sum(double x, int32_t lp) {
   for (int k = 1; k < 1 << lp; k <<= 1) x += __shfl_xor(x, k);
   return x;
 }
+
+// one over the root of a row's mean square; again in 64 bits where the squares leave 32
+__device__ __forceinline__ float one_of_large(const float (&a)[4], const float (&b)[4], int32_t lp, const RotateView& rv) {
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = fma((double)a[i], (double)a[i], fma((double)b[i], (double)b[i], sum));
+  return (float)(1.0 / sqrt(row_sum(sum, lp) / rv.d + rv.eps));
+}
+__device__ __forceinline__ float one_over_root(const float (&a)[4], const float (&b)[4], int32_t lp, const RotateView& rv) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = fmaf(a[i], a[i], fmaf(b[i], b[i], sum));
+  sum = row_sum(sum, lp);
+  return sum == INFINITY ? one_of_large(a, b, lp, rv) : rsqrtf(sum * (1.f / (float)rv.d) + rv.eps);
+}
+
+constexpr int kAhead = 2;                      // rows of a lane on their way at once
 
 }  // namespace rotate_detail
 

@@ -20,16 +20,23 @@ __device__ __forceinline__ void fill_table(float2* table, const RotateView& rv, 
     table[i] = make_float2(c, s);
   }
 }
-
-// one over the root of a row's mean square where the squares leave fp32
-__device__ __forceinline__ float one_of_large(const float (&x)[8], int32_t lp, const RotateView& rv) {
-  double sum = 0.0;
+// a lane's four of them
+template <int KIND>
+__device__ __forceinline__ void read_table(const float2* table, const Pairs<KIND>& pr, int32_t sub, float (&c)[4], float (&s)[4]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
-  return (float)(1.0 / sqrt(row_sum(sum, lp) / rv.d + rv.eps));
+  for (int i = 0; i < 4; ++i) {
+    c[i] = 1.f;
+    s[i] = 0.f;
+    if (pr.turned(i)) {
+      const float2 v = table[sub * pr.half + pr.q0 + i];
+      c[i] = v.x;
+      s[i] = v.y;
+    }
+  }
 }
 
-// A workgroup takes 2^lt positions and a block of q's or k's heads, (256 / P) >> lt of them at a time.  Bound by memory.
+// A workgroup takes 2^lt positions and a block of q's or k's heads, (256 / P) >> lt of them side by side, a lane's rows two at a time.
+
 template <typename T, int KIND>
 __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
   __shared__ float2 table[kRotateTable];
@@ -41,59 +48,64 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
   const int32_t token0 = tile << lt, sub = grp & ((1 << lt) - 1), token = token0 + sub, step = (kRotateThreads >> lp) >> lt;
   fill_table(table, rv, a.positions, a.tokens, a.t, token0, lt);
   __syncthreads();
-  const bool in = 8 * lane < rv.d, there = token < a.tokens && (!a.positions || a.positions[min(token, a.tokens - 1)] >= 0);
-  const Partners<KIND> pr{8 * lane, rv.r / 2, rv.r};
-  float c[8], s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    c[i] = 1.f;
-    s[i] = 0.f;
-    if (in && pr.turned(i)) {
-      const float2 v = table[sub * (rv.r / 2) + pr.pair(i)];
-      c[i] = v.x;
-      s[i] = pr.second(i) ? v.y : -v.y;
-    }
-  }
+  const Pairs<KIND> pr{4 * lane, rv.r / 2, rv.r, rv.d};
+  const bool active = pr.in() && token < a.tokens && (!a.positions || a.positions[min(token, a.tokens - 1)] >= 0);
+  float c[4], s[4];
+  read_table(table, pr, sub, c, s);
+  // times the weights: y_a = one (x_a ca - x_b sb), y_b = one (x_b cb + x_a sa)
   const T* weights = (const T*)rv.w[part];
-  const bool active = in && there;
-  for (int32_t h = h0 + (grp >> lt); h < h1; h += step) {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, p[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const T* row = row_at<T>(a.in[part], active ? token : 0, h);
-    if (active) {
-      read8(row + 8 * lane, x);
-      pr.load(row, x, p);
+  const bool banks = weights && rv.ws[part];
+  float ca[4], cb[4], sa[4], sb[4];
+  auto weigh = [&](int32_t h) {
+    float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
+    if (weights && pr.in()) pr.load(weights + h * rv.ws[part], wa, wb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ca[i] = c[i] * wa[i];
+      sa[i] = s[i] * wa[i];
+      cb[i] = c[i] * wb[i];
+      sb[i] = s[i] * wb[i];
     }
-    if (rv.norm) {
-      float sum = 0.f;
+  };
+  if (!banks) weigh(0);
+  const T* in = row_at<T>(a.in[part], active ? token : 0, 0);
+  T* out = const_cast<T*>(row_at<T>(a.out[part], active ? token : 0, 0));
+  for (int32_t h = h0 + (grp >> lt); h < h1; h += kAhead * step) {
+    float xa[kAhead][4], xb[kAhead][4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-      sum = row_sum(sum, lp);
-      float one = 1.f / sqrtf(sum / (float)rv.d + rv.eps);
-      if (sum == INFINITY) one = one_of_large(x, lp, rv);
-      if (weights && in) {
-        const T* w = weights + h * rv.ws[part];
-        float own[8], other[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        read8(w + 8 * lane, own);
-        pr.load(w, own, other);
+    for (int k = 0; k < kAhead; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] *= one;
-          x[i] *= own[i];
-          p[i] *= one;
-          p[i] *= other[i];
-        }
-      } else {
+      for (int i = 0; i < 4; ++i) xa[k][i] = xb[k][i] = 0.f;
+      if (active && h + k * step < h1) pr.load(in + (h + k * step) * a.in[part].sh, xa[k], xb[k]);
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] *= one;
-          p[i] *= one;
+    for (int k = 0; k < kAhead; ++k) {
+      if (h + k * step >= h1) break;
+      if (banks) weigh(h + k * step);
+      float one = 1.f;
+      if (rv.norm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fmaf(xa[k][i], xa[k][i], fmaf(xb[k][i], xb[k][i], sum));
+        sum = row_sum(sum, lp);
+        one = rsqrtf(sum * (1.f / (float)rv.d) + rv.eps);
+        if (sum == INFINITY) {
+          const float x = one_of_large(xa[k], xb[k], lp, rv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            xa[k][i] *= x;
+            xb[k][i] *= x;
+          }
+          one = 1.f;
         }
       }
-    }
-    if (active) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = pr.turned(i) ? fmaf(x[i], c[i], p[i] * s[i]) : x[i];
-      write8(const_cast<T*>(row_at<T>(a.out[part], token, h)) + 8 * lane, x);
+      for (int i = 0; i < 4; ++i) {
+        const float ya = fmaf(xa[k][i], ca[i], -xb[k][i] * sb[i]), yb = fmaf(xb[k][i], cb[i], xa[k][i] * sa[i]);
+        xa[k][i] = one * ya;
+        xb[k][i] = one * yb;
+      }
+      if (active) pr.store(out + (h + k * step) * a.out[part].sh, xa[k], xb[k]);
     }
   }
 }
@@ -101,7 +113,7 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
 // The way back: g_n = the upstream gradient turned the other way; with xhat = x * one, one = 1 / sqrt(mean(x^2) + eps),
 //   d_w += g_n xhat (over all rows),  d_x = one * (w g_n - xhat mean(w g_n xhat)).
 // Both means are sums over the row taken side by side.  A workgroup adds up its rows' part of d_w in registers, once over its rows in LDS at
-// the end, and leaves it for rows_rotate_weights_k: no atomics, the same bits every time.  Bound by memory.
+// the end, and leaves it for rows_rotate_weights_k: no atomics, the same bits every time.
 template <typename T, int KIND>
 __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackArgs a) {
   __shared__ float2 table[kRotateTable];
@@ -112,10 +124,12 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
   const int32_t h0 = (blk - (part ? a.blocks[0] : 0)) * a.sh.hb, h1 = min(h0 + a.sh.hb, rv.heads[part]);
   const int32_t lp = a.sh.lp, lt = a.sh.lt, grp = threadIdx.x >> lp, lane = threadIdx.x & ((1 << lp) - 1);
   const int32_t sub = grp & ((1 << lt) - 1), step = (kRotateThreads >> lp) >> lt;
-  const bool in = 8 * lane < rv.d;
-  const Partners<KIND> pr{8 * lane, rv.r / 2, rv.r};
+  const Pairs<KIND> pr{4 * lane, rv.r / 2, rv.r, rv.d};
+  const bool in = pr.in(), banks = rv.ws[part] != 0;
   const T* weights = (const T*)rv.w[part];
-  float gw[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
+  if (weights && !banks && in) pr.load(weights, wa, wb);
+  float gwa[4] = {0.f, 0.f, 0.f, 0.f}, gwb[4] = {0.f, 0.f, 0.f, 0.f};
   for (int32_t k = 0; k < a.tiles; ++k) {
     const int64_t first = ((int64_t)chunk * a.tiles + k) << lt;
     if (first >= a.tokens) break;              // the same for all lanes
@@ -123,66 +137,72 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
     __syncthreads();                           // the last tile's table has been read
     fill_table(table, rv, a.positions, a.tokens, a.t, token0, lt);
     __syncthreads();
-    const bool real = token < a.tokens, there = real && (!a.positions || a.positions[token] >= 0);
-    float c[8], s[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      c[i] = 1.f;
-      s[i] = 0.f;
-      if (in && pr.turned(i)) {
-        const float2 v = table[sub * (rv.r / 2) + pr.pair(i)];
-        c[i] = v.x;
-        s[i] = pr.second(i) ? -v.y : v.y;
-      }
-    }
+    const bool real = in && token < a.tokens, active = real && (!a.positions || a.positions[token] >= 0);
+    float c[4], s[4];
+    read_table(table, pr, sub, c, s);
     const int32_t b = real ? token / a.t : 0, t = real ? token - b * a.t : 0;
-    for (int32_t h = h0 + (grp >> lt); h < h1; h += step) {
-      const int64_t at = (((int64_t)b * rv.heads[part] + h) * a.t + t) * rv.d;
-      float g[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, p[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      const bool active = in && there;
-      if (active) {
-        const float* gy = a.gy[part] + at;
-        read8(gy + 8 * lane, g);
-        pr.load(gy, g, p);
+    const int64_t at = ((int64_t)b * rv.heads[part] * a.t + t) * rv.d, head = (int64_t)a.t * rv.d;
+    const T* rows = row_at<T>(a.in[part], active ? token : 0, 0);
+    for (int32_t h = h0 + (grp >> lt); h < h1; h += kAhead * step) {
+      float ga[kAhead][4], gb[kAhead][4], xa[kAhead][4], xb[kAhead][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = pr.turned(i) ? fmaf(g[i], c[i], p[i] * s[i]) : g[i];
-      }
-      if (rv.norm) {
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-        if (active) read8(row_at<T>(a.in[part], token, h) + 8 * lane, x);
-        if (weights && in) read8(weights + h * rv.ws[part] + 8 * lane, w);
-        float sq = 0.f, dot = 0.f;
+      for (int j = 0; j < kAhead; ++j) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sq = fmaf(x[i], x[i], sq);
-          dot = fmaf(w[i] * g[i], x[i], dot);
-        }
-        sq = row_sum(sq, lp);
-        dot = row_sum(dot, lp);
-        float one = 1.f / sqrtf(sq / (float)rv.d + rv.eps);
-        if (sq == INFINITY) one = one_of_large(x, lp, rv);
-        float mean = one * dot / (float)rv.d;
-        if (sq == INFINITY) {                  // so may the other sum have been
-          dot = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) dot = fmaf(w[i] * g[i], x[i] * one, dot);
-          mean = row_sum(dot, lp) / (float)rv.d;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float hat = x[i] * one;
-          gw[i] = fmaf(g[i], hat, gw[i]);
-          g[i] = one * fmaf(w[i], g[i], -hat * mean);
+        for (int i = 0; i < 4; ++i) ga[j][i] = gb[j][i] = xa[j][i] = xb[j][i] = 0.f;
+        const int32_t hj = h + j * step;
+        if (active && hj < h1) {
+          pr.load(a.gy[part] + at + hj * head, ga[j], gb[j]);
+          if (rv.norm) pr.load(rows + hj * a.in[part].sh, xa[j], xb[j]);
         }
       }
-      if (in && real) write8(a.gx[part] + at + 8 * lane, g);                  // a row of nobody: zeros
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int32_t hj = h + j * step;
+        if (hj >= h1) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ya = ga[j][i], yb = gb[j][i];
+          ga[j][i] = fmaf(ya, c[i], yb * s[i]);
+          gb[j][i] = fmaf(yb, c[i], -ya * s[i]);
+        }
+        if (rv.norm) {
+          if (banks && in) pr.load(weights + hj * rv.ws[part], wa, wb);
+          float sq = 0.f, dot = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sq = fmaf(xa[j][i], xa[j][i], fmaf(xb[j][i], xb[j][i], sq));
+            dot = fmaf(wa[i] * ga[j][i], xa[j][i], fmaf(wb[i] * gb[j][i], xb[j][i], dot));
+          }
+          sq = row_sum(sq, lp);
+          dot = row_sum(dot, lp);
+          float one = rsqrtf(sq * (1.f / (float)rv.d) + rv.eps), mean = one * dot * (1.f / (float)rv.d);
+          if (sq == INFINITY) {                // so may the other sum be
+            one = one_of_large(xa[j], xb[j], lp, rv);
+            dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot = fmaf(wa[i] * ga[j][i], xa[j][i] * one, fmaf(wb[i] * gb[j][i], xb[j][i] * one, dot));
+            mean = row_sum(dot, lp) * (1.f / (float)rv.d);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float ha = xa[j][i] * one, hb = xb[j][i] * one;
+            gwa[i] = fmaf(ga[j][i], ha, gwa[i]);
+            gwb[i] = fmaf(gb[j][i], hb, gwb[i]);
+            ga[j][i] = one * fmaf(wa[i], ga[j][i], -ha * mean);
+            gb[j][i] = one * fmaf(wb[i], gb[j][i], -hb * mean);
+          }
+        }
+        if (real) pr.store(a.gx[part] + at + hj * head, ga[j], gb[j]);        // a row of nobody: zeros
+      }
     }
   }
   if (!a.gw[part]) return;
-  float* mine = gws + (grp * rv.d + 8 * lane);
   if (in)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mine[i] = gw[i];
+    for (int i = 0; i < 4; ++i) {
+      gws[grp * rv.d + pr.first(i)] = gwa[i];
+      gws[grp * rv.d + pr.second(i)] = gwb[i];
+    }
   __syncthreads();
   for (int32_t c = threadIdx.x; c < rv.d; c += kRotateThreads) {
     float sum = 0.f;
@@ -191,33 +211,48 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
   }
 }
 
-// The parts of a weight's gradient to one, in a fixed order, and onto what is there: a workgroup to a bank of weights.
-__global__ __launch_bounds__(1024) void rows_rotate_weights_k(RotateBackArgs a) {
-  __shared__ float sums[1024];
+// The parts of a weight's gradient to one, in a fixed order, and onto what is there: a workgroup to 32 columns of a bank of weights, lanes of
+// four columns, eight rows on their way at once.
+constexpr int kWeightThreads = 1024, kWeightCols = 32, kWeightRows = 8;
+
+__global__ __launch_bounds__(kWeightThreads) void rows_rotate_weights_k(RotateBackArgs a) {
+  constexpr int LANES = kWeightCols / 4, SIDE = kWeightThreads / LANES;
+  __shared__ __align__(16) float sums[SIDE][kWeightCols];
   const RotateView& rv = a.rv;
   // banks: q's (one, or one a head), then k's
+  const int32_t cols = (rv.d + kWeightCols - 1) / kWeightCols, bank = blockIdx.x / cols, c0 = (blockIdx.x - bank * cols) * kWeightCols;
   const int32_t banks = rv.ws[0] ? rv.heads[0] : 1;
-  const int part = (int32_t)blockIdx.x >= banks;
-  const int32_t head = blockIdx.x - (part ? banks : 0);
+  const int part = bank >= banks;
+  const int32_t head = bank - (part ? banks : 0);
   if (!a.gw[part]) return;
   const int32_t first = (part ? a.blocks[0] : 0) + (rv.ws[part] ? head : 0), rows = (rv.ws[part] ? 1 : a.blocks[part]) * a.chunks;
-  const float* at = a.parts + (int64_t)first * a.chunks * rv.d;
-  const int32_t side = 1024 / rv.d, k = threadIdx.x / rv.d, c = threadIdx.x - k * rv.d;
-  float sum = 0.f;
-  if (k < side)
-    for (int32_t i = k; i < rows; i += side) sum += at[(int64_t)i * rv.d + c];
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  if (threadIdx.x >= rv.d) return;
-  sum = 0.f;
-  for (int32_t i = 0; i < side; ++i) sum += sums[i * rv.d + threadIdx.x];
-  a.gw[part][head * rv.ws[part] + threadIdx.x] += sum;
-}
-
-int32_t lanes_log(int32_t d) {
-  int32_t lp = 0;
-  while (8 << lp < d) ++lp;
-  return lp;
+  const int32_t k = threadIdx.x / LANES, c = 4 * (threadIdx.x % LANES);
+  const float* at = a.parts + (int64_t)first * a.chunks * rv.d + c0 + c;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c0 + c < rv.d)
+    for (int32_t i = k; i < rows; i += kWeightRows * SIDE) {
+      float x[kWeightRows][4];
+#pragma unroll
+      for (int j = 0; j < kWeightRows; ++j) read4(at + (int64_t)min(i + j * SIDE, rows - 1) * rv.d, x[j]);
+#pragma unroll
+      for (int j = 0; j < kWeightRows; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += i + j * SIDE < rows ? x[j][e] : 0.f;
+    }
+  write4(&sums[k][c], sum);
+  for (int32_t n = SIDE / 2; n >= 1; n /= 2) {
+    __syncthreads();
+    if (k < n) {
+      float other[4];
+      read4(&sums[k + n][c], other);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += other[e];
+      write4(&sums[k][c], sum);
+    }
+  }
+  if (k == 0 && c0 + c < rv.d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a.gw[part][head * rv.ws[part] + c0 + c + e] += sum[e];
 }
 
 struct BackPlan { RotateShape sh; int32_t blocks[2], chunks, tiles; };
@@ -230,7 +265,7 @@ BackPlan back_plan(const RotateView& rv, int32_t tokens) {
   int64_t blocks = 0;
   for (int i = 0; i < 2; ++i) blocks += p.blocks[i] = (rv.heads[i] + p.sh.hb - 1) / p.sh.hb;
   const int64_t tiles = std::max<int64_t>(((int64_t)tokens + (1 << p.sh.lt) - 1) >> p.sh.lt, 1);
-  const int64_t most = std::max<int64_t>(8 * (int64_t)cu_count() / blocks, 1), chunks = std::min(tiles, most);
+  const int64_t most = std::max<int64_t>(16 * (int64_t)cu_count() / blocks, 1), chunks = std::min(tiles, most);
   p.tiles = (int32_t)((tiles + chunks - 1) / chunks);
   p.chunks = (int32_t)((tiles + p.tiles - 1) / p.tiles);
   return p;
@@ -246,24 +281,37 @@ void rotate_back(int dtype, const RotateBackArgs& a, unsigned grid, hipStream_t 
   if (dtype == LOCOCO_F32) rows_rotate_back_k<float, KIND><<<grid, kRotateThreads, 0, s>>>(a);
   else rows_rotate_back_k<__bf16, KIND><<<grid, kRotateThreads, 0, s>>>(a);
 }
-// workgroups of the forward pass: blocks of eight heads
-int64_t rotate_groups(const RotateView& rv, int32_t tokens) {
-  const int64_t tile = 1 << (8 - lanes_log(rv.d));
-  return (tokens + tile - 1) / tile * ((rv.heads[0] + 7) / 8 + (rv.heads[1] + 7) / 8);
+
+// How the forward pass is laid out: all 256 / P rows of a workgroup at positions of their own and 16 heads in turn, where that fills the
+// device; else a row each, one position and heads side by side.
+struct RotatePlan { RotateShape sh; int32_t blocks[2]; int64_t groups; };
+RotatePlan rotate_plan(const RotateView& rv, int32_t tokens) {
+  RotatePlan p{};
+  p.sh.lp = lanes_log(rv.d);
+  const int32_t rows = kRotateThreads >> p.sh.lp;
+  auto lay = [&](int32_t lt, int32_t hb) {
+    p.sh.lt = lt;
+    p.sh.hb = hb;
+    for (int i = 0; i < 2; ++i) p.blocks[i] = (rv.heads[i] + hb - 1) / hb;
+    p.groups = (((int64_t)tokens + (1 << lt) - 1) >> lt) * (p.blocks[0] + p.blocks[1]);
+  };
+  lay(8 - p.sh.lp, 16);
+  if (p.groups < 2 * (int64_t)cu_count()) lay(0, rows);
+  return p;
 }
 
 }  // namespace
 
-bool rows_rotate_fits(const RotateView& rv, int32_t tokens) { return rotate_groups(rv, tokens) * kRotateThreads <= 0xffffffffll; }
+bool rows_rotate_fits(const RotateView& rv, int32_t tokens) { return rotate_plan(rv, tokens).groups * kRotateThreads <= 0xffffffffll; }
 
 hipError_t launch_rows_rotate(int dtype, RotateArgs a, hipStream_t s) {
-  a.sh.lp = lanes_log(a.rv.d);
-  a.sh.lt = 8 - a.sh.lp;
-  a.sh.hb = 8;
-  for (int i = 0; i < 2; ++i) a.blocks[i] = (a.rv.heads[i] + a.sh.hb - 1) / a.sh.hb;
-  const unsigned grid = (unsigned)rotate_groups(a.rv, a.tokens);
+  const RotatePlan p = rotate_plan(a.rv, a.tokens);
+  a.sh = p.sh;
+  a.blocks[0] = p.blocks[0];
+  a.blocks[1] = p.blocks[1];
+  const unsigned grid = (unsigned)p.groups;
   switch (pair_kind(a.rv.r, a.rv.adjacent)) {
-    case kHalves8: rotate<kHalves8>(dtype, a, grid, s); break;
+    case kHalves4: rotate<kHalves4>(dtype, a, grid, s); break;
     case kHalves: rotate<kHalves>(dtype, a, grid, s); break;
     case kAdjacent: rotate<kAdjacent>(dtype, a, grid, s); break;
   }
@@ -292,13 +340,13 @@ hipError_t launch_rows_rotate_backward(int dtype, RotateBackArgs a, void* worksp
   a.parts = (float*)workspace;
   const unsigned grid = (unsigned)((p.blocks[0] + p.blocks[1]) * p.chunks);
   switch (pair_kind(a.rv.r, a.rv.adjacent)) {
-    case kHalves8: rotate_back<kHalves8>(dtype, a, grid, s); break;
+    case kHalves4: rotate_back<kHalves4>(dtype, a, grid, s); break;
     case kHalves: rotate_back<kHalves>(dtype, a, grid, s); break;
     case kAdjacent: rotate_back<kAdjacent>(dtype, a, grid, s); break;
   }
   if (a.gw[0] || a.gw[1]) {
     const unsigned banks = (unsigned)((a.rv.ws[0] ? a.rv.heads[0] : 1) + (a.rv.ws[1] ? a.rv.heads[1] : 1));
-    rows_rotate_weights_k<<<banks, 1024, 0, s>>>(a);
+    rows_rotate_weights_k<<<banks * (unsigned)((a.rv.d + kWeightCols - 1) / kWeightCols), kWeightThreads, 0, s>>>(a);
   }
   return hipGetLastError();
 }
