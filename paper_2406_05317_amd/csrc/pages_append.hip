@@ -9,6 +9,8 @@ namespace {
 
 using namespace rotate_detail;
 
+typedef __attribute__((ext_vector_type(4))) float f4;
+
 struct AppendArgs {
   PagesView pg;
   RotateView rv;
@@ -19,13 +21,13 @@ struct AppendArgs {
   const int32_t* positions;
 };
 
-// an fp32 number whose rounding to fewer bits is x's: x rounded, its last bit set where that is not x (the neighbour on x's side, then)
-__device__ __forceinline__ float to_odd(double x) {
-  const float y = (float)x;
+// Borders between codes, and between scales, have three bits behind the first: an fp32 number with others decides as the value it was rounded
+// from.  One without takes the neighbour on that value's side, unless it is that value.
+__device__ __forceinline__ bool may_be_border(float y) { return (__float_as_uint(y) << 12) == 0 && y != 0.f; }
+__device__ __forceinline__ float off_border(float y, double x) {
   const double e = x - (double)y;
-  uint32_t bits = __float_as_uint(y);
-  if ((e > 0.0 || e < 0.0) && !(bits & 1u)) bits += (e > 0.0) == (x > 0.0) ? 1u : 0xffffffffu;
-  return __uint_as_float(bits);
+  const uint32_t bits = __float_as_uint(y);
+  return may_be_border(y) && (e > 0.0 || e < 0.0) ? __uint_as_float(bits + ((e > 0.0) == (x > 0.0) ? 1u : 0xffffffffu)) : y;
 }
 
 // Keys go to 4 bits by the codes nearest to their exact values.  A value as fp32 arithmetic has it, off by some 2^-23, would now and then lie
@@ -33,7 +35,7 @@ __device__ __forceinline__ float to_odd(double x) {
 // for all heads of a position; vector instructions of 64 bits go as fast as those of 32).  A key's pairs lie half a row apart, its blocks of 32 do
 // not: it goes through LDS on the way.  A workgroup takes 2^lt positions and a block of q's, k's or v's heads.
 template <typename T, int KIND>
-__global__ __launch_bounds__(kRotateThreads) void pages_append_k(AppendArgs a) {
+__global__ __launch_bounds__(kRotateThreads, 4) void pages_append_k(AppendArgs a) {
   __shared__ double2 table[kRotateTable];
   __shared__ __align__(16) float turned[kRotateThreads * 8];
   const RotateView& rv = a.rv;
@@ -48,13 +50,20 @@ __global__ __launch_bounds__(kRotateThreads) void pages_append_k(AppendArgs a) {
   const bool real = 8 * lane < rv.d && token0 + sub < a.tokens;
   const int32_t page = slot >> pg.page_shift, prow = slot & (pg.page_rows - 1);
   const bool active = part ? real && slot >= 0 && page < pg.n_pages : real && pos >= 0;
-  auto write = [&](const float (&x)[8], int32_t h, uint8_t* codes, uint8_t* scales) {
+  // where a lane's codes go, head h0's, and its block's scale; from there by heads
+  const int64_t at = ((int64_t)(active ? page : 0) * pg.Hkv + h0 + (grp >> lt)) * pg.page_rows;
+  uint8_t* codes = (part == 2 ? pg.v_codes : pg.k_codes) + (at + prow) * (pg.d / 2) + 4 * lane;
+  uint8_t* scales = (part == 2 ? pg.v_scales : pg.k_scales) + at * (pg.d / 32) + lane / 4 * pg.page_rows + prow;
+  const int32_t codes_on = step * pg.page_rows * (pg.d / 2), scales_on = step * pg.page_rows * (pg.d / 32);
+  auto write = [&](const float (&x)[8]) {      // the next head's
     uint32_t byte;
     const uint32_t code = four_bits(x, &byte);
-    if (!active) return;
-    const int64_t at = (int64_t)page * pg.Hkv + h;
-    *(uint32_t*)(codes + (at * pg.page_rows + prow) * (pg.d / 2) + 4 * lane) = code;
-    if ((lane & 3) == 0) scales[(at * (pg.d / 32) + lane / 4) * pg.page_rows + prow] = (uint8_t)byte;
+    if (active) {
+      *(uint32_t*)codes = code;
+      if ((lane & 3) == 0) *scales = (uint8_t)byte;
+    }
+    codes += codes_on;
+    scales += scales_on;
   };
   if (part == 2) {
     const T* row = row_at<T>(a.v, active ? token : 0, 0) + 8 * lane;
@@ -68,18 +77,16 @@ __global__ __launch_bounds__(kRotateThreads) void pages_append_k(AppendArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        if (h + j * step < h1) write(x[j], h + j * step, pg.v_codes, pg.v_scales);
+        if (h + j * step < h1) write(x[j]);
     }
     return;
   }
   const Pairs<KIND> pr{4 * lane, half, rv.r, rv.d};
-  auto load = [&](const T* row, int64_t sh, int32_t h, float (&xa)[kAhead][4], float (&xb)[kAhead][4]) {
+  RawPairs<T, KIND> raw[kAhead] = {};          // rows that are left out stay zeros
+  auto load = [&](const T* row, int64_t sh, int32_t h) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xa[j][i] = xb[j][i] = 0.f;
-      if (active && h + j * step < h1) pr.load(row + (h + j * step) * sh, xa[j], xb[j]);
-    }
+    for (int j = 0; j < kAhead; ++j)
+      if (active && h + j * step < h1) pr.load(row + (h + j * step) * sh, raw[j]);
   };
   const T* weights = (const T*)rv.w[part];
   const int64_t ws = rv.ws[part];
@@ -109,9 +116,12 @@ __global__ __launch_bounds__(kRotateThreads) void pages_append_k(AppendArgs a) {
     }
     const T* row = row_at<T>(a.q, active ? token : 0, 0);
     T* out = const_cast<T*>(row_at<T>(a.qo, active ? token : 0, 0));
+    load(row, a.q.sh, h0 + (grp >> lt));
     for (int32_t h = h0 + (grp >> lt); h < h1; h += kAhead * step) {
       float xa[kAhead][4], xb[kAhead][4];
-      load(row, a.q.sh, h, xa, xb);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) pr.unpack(raw[j], xa[j], xb[j]);
+      load(row, a.q.sh, h + kAhead * step);     // the next ones, while these are at work
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const int32_t hj = h + j * step;
@@ -129,42 +139,80 @@ __global__ __launch_bounds__(kRotateThreads) void pages_append_k(AppendArgs a) {
     }
     return;
   }
-  double c[4], s[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const double2 v = pr.turned(i) ? table[sub * half + pr.q0 + i] : make_double2(1.0, 0.0);
-    c[i] = v.x;
-    s[i] = v.y;
-  }
   const T* row = row_at<T>(a.k, active ? token : 0, 0);
   float* mine = turned + grp * rv.d;
+  load(row, a.k.sh, h0 + (grp >> lt));
   for (int32_t h = h0 + (grp >> lt); h < h1; h += kAhead * step) {
-    float xa[kAhead][4], xb[kAhead][4];
-    load(row, a.k.sh, h, xa, xb);
+    RawPairs<T, KIND> now[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) now[j] = raw[j];
+    load(row, a.k.sh, h + kAhead * step);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int32_t hj = h + j * step;
       if (hj >= h1) break;
+      float xa[4], xb[4];
+      pr.unpack(now[j], xa, xb);
       if (ws && pr.in()) pr.load(weights + hj * ws, wa, wb);
       double one = 1.0;
       if (rv.norm) {
         double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum = fma((double)xa[j][i], (double)xa[j][i], fma((double)xb[j][i], (double)xb[j][i], sum));
+        for (int i = 0; i < 4; ++i) sum = fma((double)xa[i], (double)xa[i], fma((double)xb[i], (double)xb[i], sum));
         one = 1.0 / sqrt(row_sum(sum, lp) / rv.d + (double)rv.eps);
       }
-      if (pr.in())
+      double na[4], nb[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        na[i] = xa[i];
+        nb[i] = xb[i];
+      }
+      if (weights)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const double na = (double)xa[j][i] * (double)wa[i], nb = (double)xb[j][i] * (double)wb[i];
-          mine[pr.first(i)] = to_odd(one * fma(na, c[i], -nb * s[i]));
-          mine[pr.second(i)] = to_odd(one * fma(nb, c[i], na * s[i]));
+          na[i] *= (double)wa[i];
+          nb[i] *= (double)wb[i];
+        }
+      bool border = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double2 v = pr.turned(i) ? table[sub * half + pr.q0 + i] : make_double2(1.0, 0.0);
+        const double ya = fma(na[i], v.x, -nb[i] * v.y), yb = fma(nb[i], v.x, na[i] * v.y);
+        na[i] = rv.norm ? one * ya : ya;
+        nb[i] = rv.norm ? one * yb : yb;
+        xa[i] = (float)na[i];
+        xb[i] = (float)nb[i];
+        border |= may_be_border(xa[i]) || may_be_border(xb[i]);
+      }
+      if (border)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          xa[i] = off_border(xa[i], na[i]);
+          xb[i] = off_border(xb[i], nb[i]);
+        }
+      if (pr.in())
+#pragma unroll
+        for (int i = 0; i < (KIND == kHalves4 ? 1 : 4); ++i) {
+          if constexpr (KIND == kHalves4) {
+            *(f4*)(mine + pr.first(0)) = f4{xa[0], xa[1], xa[2], xa[3]};
+            *(f4*)(mine + pr.second(0)) = f4{xb[0], xb[1], xb[2], xb[3]};
+          } else {
+            mine[pr.first(i)] = xa[i];
+            mine[pr.second(i)] = xb[i];
+          }
         }
       __builtin_amdgcn_wave_barrier();           // a row's lanes share a wave
       float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (pr.in()) read8(mine + 8 * lane, x);
+      if (pr.in()) {
+        const f4 lo = *(const f4*)(mine + 8 * lane), hi = *(const f4*)(mine + 8 * lane + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = lo[i];
+          x[4 + i] = hi[i];
+        }
+      }
       __builtin_amdgcn_wave_barrier();
-      write(x, hj, pg.k_codes, pg.k_scales);
+      write(x);
     }
   }
 }
@@ -187,7 +235,8 @@ AppendPlan append_plan(const PagesView& pg, int32_t tokens) {
     p.blocks_kv = (pg.Hkv + hb - 1) / hb;
     p.groups = (((int64_t)tokens + (1 << lt) - 1) >> lt) * (p.blocks_q + 2 * p.blocks_kv);
   };
-  lay(8 - p.sh.lp, 16);
+  lay(8 - p.sh.lp, 32);
+  if (p.groups < 4 * (int64_t)cu_count()) lay(8 - p.sh.lp, 16);
   if (p.groups < 2 * (int64_t)cu_count()) lay(0, kRotateThreads >> p.sh.lp);
   return p;
 }

@@ -18,8 +18,8 @@ __device__ __forceinline__ uint32_t four_bits(const float (&x)[8], uint32_t* sca
   uint32_t top = 0;                            // magnitudes as whole numbers: their order, with infinities and NaN on top
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, true));       // lanes 1, 0, 3, 2 of four
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, true));       // lanes 2, 3, 0, 1
   const int32_t e = (int32_t)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
   const uint32_t byte = top >= 0x7f800000u ? 255u : (uint32_t)(min(max(e, kMinExp), kMaxExp) + 127);
   uint32_t code = 0;

@@ -116,6 +116,16 @@ enum PairKind {
   kHalves,                                     // any other r; the rest two by two
   kAdjacent                                    // channels 2 q and 2 q + 1
 };
+// a lane's eight channels as they were loaded: what waits for its turn takes no more registers than it has bytes
+template <typename T, int KIND>
+struct RawPairs {
+  typename std::conditional<std::is_same<T, float>::value, f4_any, w2>::type a, b;
+};
+template <typename T>
+struct RawPairs<T, kHalves> {
+  T a[4], b[4];
+};
+
 template <int KIND>
 struct Pairs {
   int32_t q0, half, r, d;
@@ -148,6 +158,48 @@ struct Pairs {
         a[i] = (float)row[first(i)];
         b[i] = (float)row[second(i)];
       }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, RawPairs<T, KIND>& x) const {
+    if constexpr (KIND == kHalves) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x.a[i] = row[first(i)];
+        x.b[i] = row[second(i)];
+      }
+    } else if constexpr (KIND == kHalves4) {
+      x.a = *(const decltype(x.a)*)(row + first(0));
+      x.b = *(const decltype(x.b)*)(row + second(0));
+    } else if constexpr (std::is_same<T, float>::value) {
+      x.a = *(const f4_any*)(row + 2 * q0);
+      x.b = *(const f4_any*)(row + 2 * q0 + 4);
+    } else {
+      const w4 v = *(const w4*)(row + 2 * q0);
+      x.a = w2{v[0], v[1]};
+      x.b = w2{v[2], v[3]};
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void unpack(const RawPairs<T, KIND>& x, float (&a)[4], float (&b)[4]) const {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (KIND == kHalves) {
+        y[i] = (float)x.a[i];
+        y[4 + i] = (float)x.b[i];
+      } else if constexpr (std::is_same<T, float>::value) {
+        y[i] = x.a[i];
+        y[4 + i] = x.b[i];
+      } else {
+        y[i] = __uint_as_float(i & 1 ? x.a[i / 2] & 0xffff0000u : x.a[i / 2] << 16);
+        y[4 + i] = __uint_as_float(i & 1 ? x.b[i / 2] & 0xffff0000u : x.b[i / 2] << 16);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = KIND == kAdjacent ? y[2 * i] : y[i];
+      b[i] = KIND == kAdjacent ? y[2 * i + 1] : y[4 + i];
     }
   }
   template <typename T>

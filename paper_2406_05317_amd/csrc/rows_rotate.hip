@@ -211,9 +211,9 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
   }
 }
 
-// The parts of a weight's gradient to one, in a fixed order, and onto what is there: a workgroup to 32 columns of a bank of weights, lanes of
+// The parts of a weight's gradient to one, in a fixed order, and onto what is there: a workgroup to 16 columns of a bank of weights, lanes of
 // four columns, eight rows on their way at once.
-constexpr int kWeightThreads = 1024, kWeightCols = 32, kWeightRows = 8;
+constexpr int kWeightThreads = 1024, kWeightCols = 16, kWeightRows = 8;
 
 __global__ __launch_bounds__(kWeightThreads) void rows_rotate_weights_k(RotateBackArgs a) {
   constexpr int LANES = kWeightCols / 4, SIDE = kWeightThreads / LANES;
