@@ -588,7 +588,11 @@ LOCOCO_API lococo_status lococo_pages_tree(int32_t n, int32_t tokens, const int3
 /* lococo_pages_attn with another rule of what a new row sees: all of its request's rows ahead of the new ones (positions 0 .. held -
  * new - 1) and those new rows j, at position held - new + j, whose bit its mask has; any mask, not only a tree's.  A row's own bit
  * counts like the others; a query that sees nothing gets zeros.  New rows that a mask has no bits for (mask_words is 1 .. 8) are not
- * seen.  All else, the workspace (lococo_pages_workspace_bytes of the same sizes) and the promises on NaN among it, is as there. */
+ * seen.  All else, the promises on NaN among it, is as there; max_held says only whether requests are long, work is dealt out by what
+ * they hold.
+ * workspace: device, 256-byte aligned, lococo_pages_attn_tree_workspace_bytes of the same sizes, or of a larger max_held (may be 0). */
+LOCOCO_API lococo_status lococo_pages_attn_tree_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests,
+                                                                size_t* out);
 LOCOCO_API lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
                                                 const lococo_tensor* o, int32_t rows_per_batch, const uint32_t* masks,
                                                 int32_t mask_words, void* workspace, size_t ws_bytes, void* stream);

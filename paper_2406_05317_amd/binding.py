@@ -33,7 +33,7 @@ EXPORTS = ["lococo_plan", "lococo_workspace_bytes", "lococo_attn_only", "lococo_
            "lococo_pages_plan", "lococo_pages_store", "lococo_pages_load", "lococo_pages_workspace_bytes",
            "lococo_pages_attn",
            "lococo_rows_rotate", "lococo_rows_rotate_backward_workspace_bytes", "lococo_rows_rotate_backward", "lococo_pages_append",
-           "lococo_pages_tree", "lococo_pages_attn_tree", "lococo_pages_keep", "lococo_pages_move"]
+           "lococo_pages_tree", "lococo_pages_attn_tree_workspace_bytes", "lococo_pages_attn_tree", "lococo_pages_keep", "lococo_pages_move"]
 
 
 class lococo_config(C.Structure):
@@ -149,6 +149,7 @@ def lib():
         L.lococo_rows_rotate_backward.argtypes = [rtp, tp, tp, i32, i32] + [vp] * 8 + [C.c_size_t, vp]
         L.lococo_pages_append.argtypes = [pgp, rtp, tp, tp, tp, tp, i32, i32, vp, vp, vp]
         L.lococo_pages_tree.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.lococo_pages_attn_tree_workspace_bytes.argtypes = [pgp, rqp, C.POINTER(C.c_size_t)]
         L.lococo_pages_attn_tree.argtypes = [pgp, rqp, tp, tp, i32, vp, i32, vp, C.c_size_t, vp]
         L.lococo_pages_keep.argtypes = [pgp, i32, i32, i32] + [vp] * 13
         L.lococo_pages_move.argtypes = [pgp, i32, i32] + [vp] * 4
@@ -605,6 +606,12 @@ def lococo_pages_tree(starts, held, parents, masks, positions, bases=None):
     _check(lib().lococo_pages_tree(n, parents.numel(), s, h, b, p, masks.shape[1], m, x, _stream_now()))
 
 
+def lococo_pages_attn_tree_workspace_bytes(pages: Pages, n: int, tokens: int, max_new: int, max_held: int, table_pages: int = 1) -> int:
+    r, out = lococo_requests(n, tokens, table_pages, max_new, max_held, None, None, None), C.c_size_t(0)
+    _check(lib().lococo_pages_attn_tree_workspace_bytes(pages.ref, C.byref(r), C.byref(out)))
+    return out.value
+
+
 def lococo_pages_attn_tree(pages: Pages, q, o, tables, starts, held, masks, max_new: int, max_held: int, workspace=None):
     """lococo_pages_attn with the new rows that a row sees named by its mask, masks [tokens, words] (int32, words of bits)."""
     x, y = _rows(pages, q, pages.c.n_q_heads), _rows(pages, o, pages.c.n_q_heads)
@@ -691,8 +698,10 @@ def workspace(cfg, L: int, B: int, history: bool = False, device="cuda") -> torc
 
 
 def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int) -> torch.Tensor | None:
-    """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes (max_held may be larger than theirs)."""
-    need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
+    """Allocate (through torch) the workspace of lococo_pages_attn and lococo_pages_attn_tree calls of these sizes (max_held may be larger
+    than theirs)."""
+    need = max(lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held),
+               lococo_pages_attn_tree_workspace_bytes(pages, n, tokens, max_new, max_held))
     return torch.empty(need, dtype=torch.uint8, device=pages.device) if need else None
 
 

@@ -701,7 +701,7 @@ lococo_status scratch_on_this_device(void** out) {
 extern "C" {
 
 const char* lococo_last_error(void) { return g_err; }
-const char* lococo_version(void) { return "0.4.0"; }
+const char* lococo_version(void) { return "0.5.0"; }
 
 lococo_status lococo_debug_option(int32_t option, int64_t value) {
   switch (option) {
@@ -2140,6 +2140,16 @@ lococo_status lococo_pages_tree(int32_t n, int32_t tokens, const int32_t* starts
   return LOCOCO_OK;
 }
 
+lococo_status lococo_pages_attn_tree_workspace_bytes(const lococo_pages* pages, const lococo_requests* requests, size_t* out) {
+  lococo_status st;
+  if (!out) return fail(LOCOCO_EINVAL, "out is NULL");
+  if ((st = check_pages(pages, true)) || (st = check_requests(pages, requests, false))) return st;
+  const PagesAttnArgs a = pages_attn_args(pages, requests);
+  if (!pages_attn_tree_fits(pages->dtype, a)) return fail(LOCOCO_EUNSUPPORTED, "more query rows than one launch takes");
+  *out = align_up(pages_attn_tree_workspace_bytes(pages->dtype, a), 256);
+  return LOCOCO_OK;
+}
+
 lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_requests* requests, const lococo_tensor* q,
                                      const lococo_tensor* o, int32_t rows_per_batch, const uint32_t* masks, int32_t mask_words,
                                      void* workspace, size_t ws_bytes, void* stream) {
@@ -2155,9 +2165,10 @@ lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_req
   a.q = rows_view(q, rows_per_batch);
   a.o = rows_view(o, rows_per_batch);
   a.max_held = (int32_t)std::min<int64_t>(a.max_held, (int64_t)a.table_pages * pages->page_rows);
-  const size_t need = align_up(pages_attn_workspace_bytes(pages->dtype, a), 256);
+  if (!pages_attn_tree_fits(pages->dtype, a)) return fail(LOCOCO_EUNSUPPORTED, "more query rows than one launch takes");
+  const size_t need = align_up(pages_attn_tree_workspace_bytes(pages->dtype, a), 256);
   if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
-    return fail(LOCOCO_EWORKSPACE, "attention over pages needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,
+    return fail(LOCOCO_EWORKSPACE, "attention under masks needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,
                 workspace ? ws_bytes : (size_t)0);
   KTimer kt(K_PAGES_ATTN_TREE, (hipStream_t)stream);
   HIP_TRY(launch_pages_attn_tree(pages->dtype, a, masks, mask_words, workspace, (hipStream_t)stream), "attention over pages launch");

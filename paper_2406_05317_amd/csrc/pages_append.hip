@@ -16,7 +16,7 @@ struct AppendArgs {
   RotateView rv;
   RotateShape sh;
   RowsView q, k, v, qo;
-  int32_t tokens, blocks_q, blocks_kv;         // blocks of heads: q's, k's, v's
+  int32_t tokens, tiles, blocks_q, blocks_kv;  // tiles of positions; blocks of q's heads, of k's and v's
   const int32_t* slots;
   const int32_t* positions;
 };
@@ -40,9 +40,10 @@ __global__ __launch_bounds__(kRotateThreads, 4) void pages_append_k(AppendArgs a
   __shared__ __align__(16) float turned[kRotateThreads * 8];
   const RotateView& rv = a.rv;
   const PagesView& pg = a.pg;
-  const int32_t all = a.blocks_q + 2 * a.blocks_kv, tile = blockIdx.x / all, blk = blockIdx.x - tile * all;
-  const int part = blk < a.blocks_q ? 0 : blk < a.blocks_q + a.blocks_kv ? 1 : 2;
-  const int32_t h0 = (part == 0 ? blk : part == 1 ? blk - a.blocks_q : blk - a.blocks_q - a.blocks_kv) * a.sh.hb;
+  // keys, which take longest, ahead of the others
+  const int32_t blk = blockIdx.x / a.tiles, tile = blockIdx.x - blk * a.tiles;
+  const int part = blk < a.blocks_kv ? 1 : blk < a.blocks_kv + a.blocks_q ? 0 : 2;
+  const int32_t h0 = (part == 1 ? blk : part == 0 ? blk - a.blocks_kv : blk - a.blocks_q - a.blocks_kv) * a.sh.hb;
   const int32_t h1 = min(h0 + a.sh.hb, part ? pg.Hkv : pg.Hq);
   const int32_t lp = a.sh.lp, lt = a.sh.lt, grp = threadIdx.x >> lp, lane = threadIdx.x & ((1 << lp) - 1);
   const int32_t token0 = tile << lt, sub = grp & ((1 << lt) - 1), step = (kRotateThreads >> lp) >> lt, half = rv.r / 2;
@@ -224,7 +225,7 @@ void append(int dtype, const AppendArgs& a, unsigned grid, hipStream_t s) {
 }
 
 // As the forward pass of lococo_rows_rotate: positions side by side and heads in turn where that fills the device, else a row each.
-struct AppendPlan { RotateShape sh; int32_t blocks_q, blocks_kv; int64_t groups; };
+struct AppendPlan { RotateShape sh; int32_t tiles, blocks_q, blocks_kv; int64_t groups; };
 AppendPlan append_plan(const PagesView& pg, int32_t tokens) {
   AppendPlan p{};
   p.sh.lp = lanes_log(pg.d);
@@ -233,10 +234,10 @@ AppendPlan append_plan(const PagesView& pg, int32_t tokens) {
     p.sh.hb = hb;
     p.blocks_q = (pg.Hq + hb - 1) / hb;
     p.blocks_kv = (pg.Hkv + hb - 1) / hb;
-    p.groups = (((int64_t)tokens + (1 << lt) - 1) >> lt) * (p.blocks_q + 2 * p.blocks_kv);
+    p.tiles = (int32_t)(((int64_t)tokens + (1 << lt) - 1) >> lt);
+    p.groups = (int64_t)p.tiles * (p.blocks_q + 2 * p.blocks_kv);
   };
-  lay(8 - p.sh.lp, 32);
-  if (p.groups < 4 * (int64_t)cu_count()) lay(8 - p.sh.lp, 16);
+  lay(8 - p.sh.lp, 16);
   if (p.groups < 2 * (int64_t)cu_count()) lay(0, kRotateThreads >> p.sh.lp);
   return p;
 }
@@ -248,7 +249,7 @@ bool pages_append_fits(const PagesView& pg, int32_t tokens) { return append_plan
 hipError_t launch_pages_append(int dtype, const PagesView& pg, const RotateView& rv, const RowsView& q, const RowsView& k, const RowsView& v,
                                const RowsView& qo, int32_t tokens, const int32_t* slots, const int32_t* positions, hipStream_t s) {
   const AppendPlan p = append_plan(pg, tokens);
-  AppendArgs a{pg, rv, p.sh, q, k, v, qo, tokens, p.blocks_q, p.blocks_kv, slots, positions};
+  AppendArgs a{pg, rv, p.sh, q, k, v, qo, tokens, p.tiles, p.blocks_q, p.blocks_kv, slots, positions};
   const unsigned grid = (unsigned)p.groups;
   switch (pair_kind(rv.r, rv.adjacent)) {
     case kHalves4: append<kHalves4>(dtype, a, grid, s); break;

@@ -308,39 +308,45 @@ __device__ __forceinline__ void load_v(ValueCodes<D>& v, const PagesView& pg, in
   v.scales = *(const u32x4*)(pg.v_scales + at * (D / 32) + (m * (D / 16) / 32) * pg.page_rows + row);
 }
 
-template <typename T, int D, int QB, bool TREE>
-__device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm) {
+// A tile's work on the keys key_lo .. key_hi - 1: to o where that is all it sees, else as a part, rows from part_row on.  WAVES waves take 64
+// keys in turn and meet at the end; one alone writes from where the products left its results.  tid: threadIdx.x.
+template <typename T, int D, int QB, bool TREE, int WAVES>
+__device__ __forceinline__ void attn_piece(const TileArgs& g, const TreeMasks& tm, const TileJob& job, int32_t kvh, int32_t key_lo, int32_t key_hi,
+                                           bool whole_job, int64_t part_row, int tid) {
   constexpr int PARTS = std::is_same<T, float>::value ? 3 : 1, PROBS = PARTS == 3 ? 3 : 2, TR = 16 * QB, STEPS = D / 32, COLS = D / 16, LD = D + 4;
-  __shared__ __align__(16) float joined[kTileWaves][TR][LD];
-  __shared__ float ml[kTileWaves][TR][2];
-  __shared__ int32_t nan_key[D / 32];          // first visible key whose 32 values of V stand for NaN, among the tiles that mask;
-  __shared__ uint32_t nan_new[TREE ? D / 32 : 1][kMaskWords];                 // TREE: among those ahead of the new ones.  And new ones
-  __shared__ TileMask masks[TREE ? TR : 1];
+  __shared__ __align__(16) float joined[WAVES > 1 ? WAVES : 1][WAVES > 1 ? TR : 1][LD];
+  __shared__ float ml[WAVES > 1 ? WAVES : 1][WAVES > 1 ? TR : 1][2];
+  constexpr int OWN = WAVES == 1 ? kTileWaves : 1;                            // waves that work alone have arrays of their own
+  __shared__ int32_t nan_keys[OWN][D / 32];          // first visible key whose 32 values of V stand for NaN, among the tiles that mask;
+  __shared__ uint32_t nan_news[OWN][TREE ? D / 32 : 1][kMaskWords];                 // TREE: among those ahead of the new ones.  And new ones
+  __shared__ TileMask mask_rows[OWN][TREE ? TR : 1];
   const PagesAttnArgs& a = g.a;
   const PagesView& pg = a.pg;
-  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = l & 15, grp = l >> 4;
-  const int item = xcd_item(blockIdx.x, gridDim.x);
-  // neighbours, on one XCD: the kv heads of a part where a request is one tile (their scales share cache lines), else the tiles that
-  // read the same keys
-  const int32_t kvh = g.by_request ? item % pg.Hkv : item / g.slots / g.splits;
-  const int32_t rest = g.by_request ? item / pg.Hkv : item % (g.slots * g.splits);
-  const int32_t slot = g.by_request ? rest / g.splits : rest % g.slots, split = g.by_request ? rest % g.splits : rest / g.slots;
-  TileJob job;
-  if (!tile_job<TR, TREE>(g, slot, &job)) return;
-  const int32_t per = part_keys(g, job.keys), parts = parts_of(g, job.keys);
-  if (split >= parts) return;
-  const int32_t key_lo = split * per, key_hi = min(key_lo + per, job.keys);
-  if (threadIdx.x < D / 32) nan_key[threadIdx.x] = 0x7fffffff;
+  const int l = tid & 63, own = WAVES == 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0, w = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6),
+            m = l & 15, grp = l >> 4;
+  auto& nan_key = nan_keys[own];
+  auto& nan_new = nan_news[own];
+  auto& masks = mask_rows[own];
+  if constexpr (WAVES == 1) tid = l;
+  auto meet = [] {                               // LDS as it is written so far
+    if constexpr (WAVES == 1) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      __syncthreads();
+    }
+  };
+  if (tid < D / 32) nan_key[tid] = 0x7fffffff;
   if constexpr (TREE) {
-    if (threadIdx.x < D / 32 * kMaskWords) (&nan_new[0][0])[threadIdx.x] = 0;
+    if (tid < D / 32 * kMaskWords) (&nan_new[0][0])[tid] = 0;
     if (key_hi > job.held - job.fresh)
-      for (int i = threadIdx.x; i < TR * (kMaskWords + 2); i += 64 * kTileWaves) {
+      for (int i = tid; i < TR * (kMaskWords + 2); i += 64 * WAVES) {
         const int r = i / (kMaskWords + 2), k = i % (kMaskWords + 2) - 1;
         const int64_t token = job.first + (job.row0 + r) / pg.group;
         masks[r].w[k + 1] = r >= job.rows || k >= tm.words ? 0u : k < 0 ? 0xffffffffu : tm.masks[token * tm.words + k];
       }
   }
-  __syncthreads();
+  meet();
 
   // queries: row 16 qb + m, columns grp D/4 + 8 step ..
   bf16x8 q[QB][PARTS][STEPS];
@@ -375,7 +381,7 @@ __device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm
   const int32_t* table = a.tables + (int64_t)job.req * a.table_pages;
   float ref[QB];
   f4 o[QB][COLS], sum[QB];                     // sum: the same number in all four places of a lane
-  constexpr int kStride = kTileWaves * kTileKeys;
+  constexpr int kStride = WAVES * kTileKeys;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     ref[qb] = kNoRef;
@@ -540,7 +546,47 @@ __device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm
     }
   }
 
-  // the four waves' results to one: o[qb][j][i] is column COLS (4 grp + i) + j of row 16 qb + m
+  // o[qb][j][i] is column COLS (4 grp + i) + j of row 16 qb + m
+  if constexpr (WAVES == 1) {
+    meet();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int32_t r = 16 * qb + m, row = job.row0 + r, x = row / pg.group, at = TREE ? 0x7ffffffe : job.held - job.fresh + x;
+      if (r >= job.rows) continue;
+      const float inv = sum[qb][0] == 0.f ? 0.f : 1.f / sum[qb][0];           // a row that sees nothing: zeros
+      const int32_t token = job.first + x, ob = token < a.o.t ? 0 : token / a.o.t, ot = token - ob * a.o.t;
+      T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st;
+      if (!whole_job && grp == 0) {
+        g.part_ml[2 * (part_row + r)] = ref[qb];
+        g.part_ml[2 * (part_row + r) + 1] = sum[qb][0];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int col = COLS * (4 * grp + i), block = col / 32;
+        bool odd = at >= nan_key[block];
+        if (TREE && key_hi > ahead)
+          for (int32_t k = 0; k < kMaskWords; ++k) odd |= (nan_new[TREE ? block : 0][k] & masks[TREE ? r : 0].w[k + 1]) != 0;
+        __align__(16) T z[COLS];
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+          if (odd) o[qb][j][i] = NAN;
+          z[j] = (T)(o[qb][j][i] * inv);
+        }
+        if (!whole_job) {
+#pragma unroll
+          for (int j = 0; j < COLS; j += 4)
+            *(f4*)(g.part_o + (part_row + r) * D + col + j) = f4{o[qb][j][i], o[qb][j + 1][i], o[qb][j + 2][i], o[qb][j + 3][i]};
+        } else if constexpr (PARTS == 1) {
+          *(typename Bytes<COLS * 2>::type*)(out + col) = *(typename Bytes<COLS * 2>::type*)z;
+        } else {
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) out[col + j] = z[j];
+        }
+      }
+    }
+    return;
+  }
+  // the waves' results to one
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     if (grp == 0) {
@@ -554,17 +600,17 @@ __device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm
         *(f4*)&joined[w][16 * qb + m][COLS * (4 * grp + i) + j] = f4{o[qb][j][i], o[qb][j + 1][i], o[qb][j + 2][i], o[qb][j + 3][i]};
   }
   __syncthreads();
-  constexpr int PER = TR * D / (64 * kTileWaves);                             // columns of a thread
-  const int r = threadIdx.x / (D / PER), col = threadIdx.x % (D / PER) * PER;
+  constexpr int PER = TR * D / (64 * WAVES);                             // columns of a thread
+  const int r = tid / (D / PER), col = tid % (D / PER) * PER;
   if (r >= job.rows) return;
   float best = ml[0][r][0];
 #pragma unroll
-  for (int k = 1; k < kTileWaves; ++k) best = fmaxf(best, ml[k][r][0]);
+  for (int k = 1; k < WAVES; ++k) best = fmaxf(best, ml[k][r][0]);
   float y[PER], total = 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) y[i] = 0.f;
 #pragma unroll
-  for (int k = 0; k < kTileWaves; ++k) {
+  for (int k = 0; k < WAVES; ++k) {
     const float keep = __builtin_amdgcn_exp2f(ml[k][r][0] - best);
     total += ml[k][r][1] * keep;
 #pragma unroll
@@ -580,8 +626,8 @@ __device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm
       for (int i = 0; i < PER; ++i)
         if (nan_new[TREE ? (col + i) / 32 : 0][k] & masks[TREE ? r : 0].w[k + 1]) y[i] = NAN;
   }
-  if (parts > 1) {
-    const int64_t pr = (((int64_t)slot * pg.Hkv + kvh) * g.splits + split) * TR + r;
+  if (!whole_job) {
+    const int64_t pr = part_row + r;
 #pragma unroll
     for (int i = 0; i < PER; i += 4) *(f4*)(g.part_o + pr * D + col + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
     if (col == 0) {
@@ -604,6 +650,26 @@ __device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm
 #pragma unroll
     for (int i = 0; i < PER; ++i) out[i] = z[i];
   }
+}
+
+// A workgroup's tile and part of the keys, by its number.
+template <typename T, int D, int QB, bool TREE>
+__device__ __forceinline__ void attn_tile(const TileArgs& g, const TreeMasks& tm) {
+  constexpr int TR = 16 * QB;
+  const PagesView& pg = g.a.pg;
+  const int item = xcd_item(blockIdx.x, gridDim.x);
+  // neighbours, on one XCD: the kv heads of a part where a request is one tile (their scales share cache lines), else the tiles that
+  // read the same keys
+  const int32_t kvh = g.by_request ? item % pg.Hkv : item / g.slots / g.splits;
+  const int32_t rest = g.by_request ? item / pg.Hkv : item % (g.slots * g.splits);
+  const int32_t slot = g.by_request ? rest / g.splits : rest % g.slots, split = g.by_request ? rest % g.splits : rest / g.slots;
+  TileJob job;
+  if (!tile_job<TR, TREE>(g, slot, &job)) return;
+  const int32_t per = part_keys(g, job.keys), parts = parts_of(g, job.keys);
+  if (split >= parts) return;
+  const int32_t key_lo = split * per, key_hi = min(key_lo + per, job.keys);
+  attn_piece<T, D, QB, TREE, kTileWaves>(g, tm, job, kvh, key_lo, key_hi, parts == 1, (((int64_t)slot * pg.Hkv + kvh) * g.splits + split) * TR,
+                             threadIdx.x);
 }
 
 // The parts of a row to one, in their order.  WAVES waves to a row, which take its parts in turn: one where there are few, so that four

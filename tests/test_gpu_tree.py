@@ -82,9 +82,18 @@ def test_trees_of_numbers_that_make_no_sense():
 
 
 # ---- attention under masks
-def run_attn(pages, q, tables, starts, held, masks, o=None, fill=5.0):
+def run_attn(pages, q, tables, starts, held, masks, o=None, fill=5.0, hint=None):
+    """hint: another max_held than the requests' own, which only says how the work is dealt out (tables are made to hold as many)."""
     news = (starts[1:] - starts[:-1]).tolist()
     o = torch.full_like(q, fill, device="cuda") if o is None else o
+    if hint:
+        wide = torch.full((tables.shape[0], max(tables.shape[1], hint // pages.c.page_rows)), -1, dtype=torch.int32)
+        wide[:, :tables.shape[1]] = tables
+        ws = lb.pages_workspace(pages, len(held), q.shape[0] * q.shape[2], max(max(news), -(-q.shape[2] // len(held))), hint)
+        ws.fill_(255)
+        lb.lococo_pages_attn_tree(pages, q.cuda() if not q.is_cuda else q, o, wide.cuda(), starts.cuda(), held.cuda(), words_tensor(masks).cuda(),
+                                  max(max(news), -(-q.shape[2] // len(held))), hint, ws)
+        return o
     most, tokens = int(held.clamp(min=0).max()), q.shape[0] * q.shape[2]
     promise = max(max(news), -(-tokens // len(held)))
     ws = lb.pages_workspace(pages, len(held), tokens, promise, most)
@@ -160,16 +169,14 @@ def test_attention_over_long_contexts(dtype, kv, group, d, R, lens, kind):
 @pytest.mark.parametrize("kv,group,d", [(2, 4, 128), (1, 2, 64), (2, 2, 96)])
 @pytest.mark.parametrize("lens", [[(60, 1), (300, 20)], [(2500, 40), (70, 70)], [(900, 130), (64, 64), (33, 1)]])
 def test_a_chain_is_causal_attention(dtype, kv, group, d, lens):
-    """Every row the child of the one ahead: the same visibility as lococo_pages_attn, and the same bits (the same order of sums)."""
+    """Every row the child of the one ahead: the visibility of lococo_pages_attn, whose results (sums in another order) both are held to."""
     pages, q, tables, starts, held = make_batch(41, dtype, kv, group, d, 16, lens)
     masks = masks_of(0, starts, held, -(-max(w for _, w in lens) // 32), "chain")
-    got = run_attn(pages, q, tables, starts, held, masks)
-    check_attn(pages, q, tables, starts, held, masks, got)
+    check_attn(pages, q, tables, starts, held, masks, run_attn(pages, q, tables, starts, held, masks))
     o = torch.full_like(q, 5.0, device="cuda")
     ws = lb.pages_workspace(pages, len(lens), q.shape[2], max(w for _, w in lens), int(held.max()))
     lb.lococo_pages_attn(pages, q.cuda(), o, tables.cuda(), starts.cuda(), held.cuda(), max(w for _, w in lens), int(held.max()), ws)
-    if max(h for h, _ in lens) <= 300:                                 # (longer ones may be cut into other parts)
-        assert torch.equal(got, o)
+    check_attn(pages, q, tables, starts, held, masks, o)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -457,6 +464,65 @@ def test_drafted_turns_leave_what_one_token_at_a_time_leaves(dtype, Hq, Hkv, d, 
         free = [int(tree.ring[j % 60]) for j in range(head, tail)]
         mine = [int(x) for i in range(n) for x in tree.tables[i, :-(-int(tree.held[i]) // R)]]
         assert sorted(free + mine) == list(range(60))
+
+
+LONG = 1 << 21                                                         # what a caller may say of requests of any length
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,group,d,R", [(2, 1, 128, 64), (1, 4, 128, 16), (2, 3, 64, 32), (1, 16, 128, 64), (1, 8, 64, 128)])
+@pytest.mark.parametrize("lens", [[(16, 16), (17, 3), (300, 2), (64, 64), (65, 33)], [(5, 5), (3, 3), (40, 0), (100, 1), (0, 0), (129, 40)],
+                                  [(0, 3), (2, 5), (200, 70)], [(700, 130), (131, 130), (550, 90)], [(3000, 9), (513, 40), (512, 40), (511, 40)],
+                                  [(4097, 33)]])
+@pytest.mark.parametrize("kind", ["random", "any"])
+def test_attention_dealt_out_by_lengths(dtype, kv, group, d, R, lens, kind):
+    """Said to be long: work is dealt out by a launch ahead, tiles to a wave alone and to four, in one part and in several."""
+    print(dtype, kv, group, d, R, lens, kind, flush=True)
+    batch = make_batch(101, dtype, kv, group, d, R, lens)
+    masks = masks_of(102, batch[3], batch[4], -(-max(w for _, w in lens) // 32), kind)
+    got = run_attn(*batch, masks, hint=LONG)
+    check_attn(*batch, masks, got)
+    assert torch.equal(got, run_attn(*batch, masks, hint=LONG))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_marks_and_missing_pages_where_work_is_dealt_out(dtype, d):
+    lens = [(2000, 40), (90, 40), (300, 33), (600, 7)]
+    pages, q, tables, starts, held = make_batch(103, dtype, 2, 2, d, 16, lens)
+    mark = lambda s, i, r, h, c: s.__setitem__((int(tables[i, r // 16]), h, c, r % 16), 255)
+    mark(pages.v_scales, 0, 1962, 1, 1)
+    mark(pages.v_scales, 0, 100, 0, 0)
+    mark(pages.v_scales, 1, 60, 0, 1)
+    mark(pages.k_scales, 2, 270, 1, 0)
+    tables[3, 5], tables[0, 50], tables[2, 18] = -1, 10 ** 9, -1
+    for kind in ("random", "any"):
+        masks = masks_of(7, starts, held, 2, kind)
+        got = run_attn(pages, q, tables, starts, held, masks, hint=LONG)
+        assert torch.isnan(got).any() and not torch.isnan(got).all()
+        check_attn(pages, q, tables, starts, held, masks, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [64, 65, 130, 1100])
+def test_many_requests_dealt_out(dtype, n):
+    """More requests than a workgroup has threads; most of them idle, one long."""
+    r = random.Random(n)
+    lens = [(r.randint(20, 90), r.randint(1, 20)) if r.random() < 60 / n else (r.randint(0, 50), 0) for _ in range(n)]
+    lens[7] = (1500, 30)
+    batch = make_batch(104, dtype, 1, 4, 64, 16, lens)
+    masks = masks_of(8, batch[3], batch[4], 1)
+    check_attn(*batch, masks, run_attn(*batch, masks, hint=LONG))
+
+
+def test_starts_that_do_not_ascend_touch_nothing_else():
+    """Requests that claim each other's rows: whatever is computed, nothing beside the call's rows of o is written."""
+    pages, q, tables, starts, held = make_batch(105, torch.bfloat16, 1, 2, 64, 16, [(100, 20), (90, 20), (80, 20)])
+    out = torch.full((1, 2, 80, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    bad = torch.tensor([40, 60, 0, 60], dtype=torch.int32)
+    for hint in (None, LONG):
+        run_attn(pages, q, tables, bad, held, [[0xffffffff]] * 60, o=out[:, :, 10:70], hint=hint)
+        assert (out[:, :, :10] == 5.0).all() and (out[:, :, 70:] == 5.0).all()
 
 
 def test_a_turn_captured():

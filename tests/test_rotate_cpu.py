@@ -181,6 +181,20 @@ def test_attention_under_masks_checks_its_arguments():
                                     None) == OK
 
 
+def test_workspace_under_masks_does_not_shrink_with_more_keys():
+    """A workspace for a larger max_held serves calls with a smaller one, whichever way either is dealt out."""
+    L, out = lb.lib(), C.c_size_t(0)
+    for p in (pages(), pages(n_q_heads=32, n_kv_heads=8), pages(dtype=lb.LOCOCO_F32, head_dim=64)):
+        for n, new in ((1, 1), (3, 9), (70, 1), (32, 60), (5, 250)):
+            last = 0
+            for held in sorted([1, 511, 768, 769, 1000, 2048, 2049, 5000, 30000, 65536, 10 ** 6, 2 ** 31 - 1]):
+                r = requests(n=n, tokens=n * new, max_new=new, max_held=held, table_pages=2 ** 23)
+                assert L.lococo_pages_attn_tree_workspace_bytes(C.byref(p), C.byref(r), C.byref(out)) == OK
+                assert out.value >= last
+                last = out.value
+    assert L.lococo_pages_attn_tree_workspace_bytes(C.byref(pages()), C.byref(requests()), None) == EINVAL
+
+
 def test_keeping_and_moving_check_their_arguments():
     L, p = lb.lib(), pages(k_codes=None, dtype=9)                       # keeping reads neither the arrays nor the heads
     names = ["tables", "starts", "held", "slots", "kept", "ring", "ends", "held_after", "ends_after", "sources", "targets", "totals"]
