@@ -17,7 +17,8 @@ __device__ __forceinline__ void rows_of(const int32_t* starts, int32_t tokens, i
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Positions and masks.  A workgroup to a request, a lane to a row: it holds the row's mask, its depth and the row it has got up to, and takes
 // over what that one holds, so that it gets twice as far up each time: as many rounds as the depth has binary digits.  The workgroups behind
-// the last request's see to the rows of nobody.  Bound by the launch.
+// the last request's see to the rows of nobody.  Bound by the launch: 3 us for 32 trees of 8 rows,
+// 5.5 for 512 of up to 64.
 template <int W>
 __global__ void pages_tree_k(PagesTreeArgs a) {
   __shared__ uint32_t bits[32 * W][W];
@@ -75,6 +76,7 @@ __global__ void pages_tree_k(PagesTreeArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Keeping.  A wave to a request: the kept rows close up, in their order, on the places its new rows have had.
+// Bound by the launches: rows 2.7 us, ring 4 us for 32 requests and 10 for 256 (one workgroup: a running sum), moving 3.3 us.
 constexpr int kKeepWaves = 4;
 
 __global__ __launch_bounds__(64 * kKeepWaves) void pages_keep_rows_k(PagesKeepArgs a) {
