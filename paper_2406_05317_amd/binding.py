@@ -310,6 +310,7 @@ class Rotation:
                                  0 if freqs is None else 2 * freqs.numel(), LOCOCO_PAIRS_ADJACENT if adjacent else LOCOCO_PAIRS_HALVES,
                                  int(norm), norm_eps, _ptr(freqs), _ptr(q_weight), _ptr(k_weight), *strides)
         self.ref = C.byref(self.c)
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
 
 
 def lococo_version() -> str:
@@ -517,42 +518,54 @@ def _whole(dtype, *arrays):
     return _here(*arrays)
 
 
-def _rotated(rot: Rotation, t: torch.Tensor, heads: int) -> lococo_tensor:
-    """View of a [b, heads, t, d] tensor of the rotation's type on the current device."""
+def _rotated(rot: Rotation, t: torch.Tensor, heads: int, dev: int) -> lococo_tensor:
+    """View of a [b, heads, t, d] tensor of the rotation's type on the current device, `dev`."""
     shape, stride = t.shape, t.stride()
-    if t.dtype is not rot.dtype or len(shape) != 4 or shape[1] != heads or shape[3] != rot.c.head_dim or stride[3] != 1:
-        raise TypeError(f"expected [b, {heads}, t, {rot.c.head_dim}] of {rot.dtype} on the device with the last axis contiguous, got "
+    if t.dtype is not rot.dtype or len(shape) != 4 or shape[1] != heads or shape[3] != rot.head_dim or stride[3] != 1 or t.get_device() != dev:
+        raise TypeError(f"expected [b, {heads}, t, {rot.head_dim}] of {rot.dtype} on the current device, {dev}, with the last axis contiguous, got "
                         f"{tuple(shape)} of {t.dtype}, {t.device}, strides {stride}")
-    return lococo_tensor(_here(t)[0], stride[0], stride[1], stride[2])
+    return lococo_tensor(t.data_ptr(), stride[0], stride[1], stride[2])
 
 
-def _rotation_here(rot: Rotation):
-    if rot.device is not None and rot.device != torch._C._cuda_getDevice():
-        raise TypeError(f"the rotation's frequencies and weights are on device {rot.device}, not on the current one")
+def _rotation_here(rot: Rotation) -> int:
+    """The current device, which the rotation's arrays have to be on (-2 where there is none: no array is there)."""
+    try:
+        dev = torch._C._cuda_getDevice()
+    except RuntimeError:
+        dev = -2
+    if rot.device is not None and rot.device != dev:
+        raise TypeError(f"the rotation's frequencies and weights are on device {rot.device}, not on the current one, {dev}")
+    return dev
 
 
-def _rotated_pair(rot: Rotation, q, k):
-    """(views of q and k by reference, batch entries, rows of one)"""
-    if q is None and k is None:
-        raise ValueError("neither q nor k is given")
-    if q is not None and k is not None and (q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]):
+def _rotated_pair(rot: Rotation, q, k, dev: int):
+    """(views of q and k, batch entries, rows of one)"""
+    if q is None:
+        if k is None:
+            raise ValueError("neither q nor k is given")
+        return None, _rotated(rot, k, rot.n_kv_heads, dev), k.shape[0], k.shape[2]
+    x = _rotated(rot, q, rot.n_q_heads, dev)
+    b, _, t, _ = q.shape
+    if k is None:
+        return x, None, b, t
+    if k.shape[0] != b or k.shape[2] != t:
         raise ValueError(f"q and k of {tuple(q.shape)} and {tuple(k.shape)} are not of the same tokens")
-    some = k if q is None else q
-    views = [None if x is None else C.byref(_rotated(rot, x, h)) for x, h in ((q, rot.c.n_q_heads), (k, rot.c.n_kv_heads))]
-    return views, some.shape[0], some.shape[2]
+    return x, _rotated(rot, k, rot.n_kv_heads, dev), b, t
 
 
 def _positions_of(positions, tokens):
-    if positions is not None and positions.numel() != tokens:
+    if positions is None:
+        return None
+    if positions.numel() != tokens:
         raise ValueError(f"{positions.numel()} positions for {tokens} rows")
     return _whole(_I32, positions)[0]
 
 
 def lococo_rows_rotate(rot: Rotation, q, k, q_out, k_out, positions=None):
     """q, k [b, heads, t, d] normed and turned by their rows' positions (None: 0 .. t - 1) into q_out, k_out; either may be None."""
-    _rotation_here(rot)
-    (x, y), b, t = _rotated_pair(rot, q, k)
-    (xo, yo), bo, to = _rotated_pair(rot, q_out, k_out)
+    dev = _rotation_here(rot)
+    x, y, b, t = _rotated_pair(rot, q, k, dev)
+    xo, yo, bo, to = _rotated_pair(rot, q_out, k_out, dev)
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (b, t) != (bo, to):
         raise ValueError("q_out, k_out do not fit q, k")
     _check(lib().lococo_rows_rotate(rot.ref, x, y, xo, yo, max(t, 1), b * t, _positions_of(positions, b * t), _stream_now()))
@@ -566,8 +579,7 @@ def lococo_rows_rotate_backward_workspace_bytes(rot: Rotation, tokens: int) -> i
 
 def lococo_rows_rotate_backward(rot: Rotation, q, k, positions, d_q_out, d_k_out, d_q, d_k, d_q_weight=None, d_k_weight=None, workspace=None):
     """Gradients of lococo_rows_rotate: fp32, contiguous; d_q, d_k overwritten (they may be d_q_out, d_k_out), the weights' added to."""
-    _rotation_here(rot)
-    (x, y), b, t = _rotated_pair(rot, q, k)
+    x, y, b, t = _rotated_pair(rot, q, k, _rotation_here(rot))
     for rows, grads in ((q, (d_q_out, d_q)), (k, (d_k_out, d_k))):
         for g in grads:
             if (g is None) != (rows is None) or (g is not None and (g.dtype is not torch.float32 or not g.is_contiguous() or g.shape != rows.shape)):
