@@ -509,7 +509,8 @@ LOCOCO_API lococo_status lococo_pages_attn(const lococo_pages* pages, const loco
  *   y_a = n_a cos(t) - n_b sin(t),  y_b = n_b cos(t) + n_a sin(t),  t = position * freqs[i]
  *
  * for the pairs i = 0 .. rotary_dim / 2 - 1 of channels (a, b); channels from rotary_dim on are n as it is.  Positions are whole
- * numbers and t is their exact product with the fp32 frequency: its cosine and sine are right to fp32 at any position. */
+ * numbers and t is their exact product with the fp32 frequency (up to 2^24 radians a position): its cosine and sine are right to fp32 at
+ * any position. */
 enum { LOCOCO_PAIRS_HALVES = 0,    /* pair i is the channels i and i + rotary_dim / 2 */
        LOCOCO_PAIRS_ADJACENT = 1   /* pair i is the channels 2 i and 2 i + 1          */ };
 typedef struct lococo_rotation {

@@ -101,11 +101,11 @@ __global__ __launch_bounds__(kRotateThreads, KIND == kHalves ? 3 : 4) void pages
     const float f = rv.freqs[i - x * half];
     if (part) {
       double s, c;
-      sincos((double)p * (double)f, &s, &c);
+      sincospi(half_turns(p, f), &s, &c);
       table[i] = make_double2(c, s);
     } else {
       float s, c;
-      sincospif(half_turns(p, f), &s, &c);
+      sincospif((float)half_turns(p, f), &s, &c);
       ((float2*)table)[i] = make_float2(c, s);
     }
   }

@@ -226,10 +226,15 @@ struct Pairs {
 };
 inline PairKind pair_kind(int32_t r, int32_t adjacent) { return adjacent ? kAdjacent : r % 8 ? kHalves : kHalves4; }
 
-// whole turns left out of the angle in 64 bits (position * frequency is exact there): half turns in [-1, 1]
-__device__ __forceinline__ float half_turns(int32_t position, float freq) {
-  const double h = (double)position * (double)freq * 0.31830988618379067154;
-  return (float)(h - 2.0 * rint(h * 0.5));
+// The angle position * freq in half turns, whole turns left out: in [-1, 1], off by some 2^-53 at any position and at
+// frequencies up to 2^24.  The product has up to 55 bits and 1 / pi has no end, so both are sums of two numbers: what a product leaves over is
+// an fma.
+__device__ __forceinline__ double half_turns(int32_t position, float freq) {
+  constexpr double kHi = 0.3183098861837907, kLo = -1.9678676675182486e-17;    // of 1 / pi
+  const double p = position, f = freq, a = p * f, h = a * kHi;
+  const double l = fma(a, kHi, -h) + fma(a, kLo, fma(p, f, -a) * kHi);
+  const double r = h - 2.0 * rint(h * 0.5) + l;
+  return r - 2.0 * rint(r * 0.5);
 }
 
 // sums over the P lanes of a row; in fp32 up to 16 lanes without a trip through the LDS crossbar
