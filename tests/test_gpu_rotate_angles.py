@@ -29,12 +29,12 @@ def left_over(positions, freqs):
     return torch.tensor(out, dtype=torch.float64)
 
 
-def far(seed, n, pairs):
-    """Positions of every size up to the largest, frequencies from 1e-4 to 1e4 radians a position."""
+def far(seed, n, pairs, least=0, low=-4):
+    """Positions of every size from 2^least up to the largest, frequencies from 10^low to 10^4 radians a position."""
     g = torch.Generator().manual_seed(seed)
-    pos = (2.0 ** (31.0 * torch.rand(n, generator=g, dtype=torch.float64))).long() - 1
+    pos = (2.0 ** (least + (31 - least) * torch.rand(n, generator=g, dtype=torch.float64))).long() - 1
     pos[:4] = torch.tensor([2 ** 31 - 1, 2 ** 30 + 12345, 2 ** 29 + 1, 2 ** 29 - 1])
-    freqs = (10.0 ** (8.0 * torch.rand(pairs, generator=g, dtype=torch.float64) - 4.0)).float()
+    freqs = (10.0 ** (low + (4 - low) * torch.rand(pairs, generator=g, dtype=torch.float64))).float()
     return pos.int(), freqs
 
 
@@ -57,11 +57,12 @@ def test_cosines_and_sines_of_far_positions(adjacent):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("adjacent", [False, True])
-def test_codes_of_far_positions(dtype, adjacent):
+@pytest.mark.parametrize("least,low", [(0, -4), (30, 3)])
+def test_codes_of_far_positions(dtype, adjacent, least, low):
     """Codes and scales of appended keys are those of the exact angles, every one (values of 64 bits: one in 10^10 lies where two exact
-    computations could take neighbours)."""
-    n, H, d, R = 128, 2, 128, 32
-    pos, freqs = far(2, n, d // 2)
+    computations could take neighbours).  Rounded products of the largest positions, off by up to 2^-9, get some of 65536 wrong."""
+    n, H, d, R = 256, 2, 128, 32
+    pos, freqs = far(2, n, d // 2, least, low)
     g = torch.Generator().manual_seed(3)
     rows = torch.randn(1, 3 * H, n, d, generator=g).to(dtype).cuda()
     rot = lb.Rotation(dtype=dtype, n_q_heads=H, n_kv_heads=H, head_dim=d, freqs=freqs.cuda(), adjacent=adjacent)
