@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kRotateThreads, KIND == kHalves ? 3 : 4) void pages
       table[i] = make_double2(c, s);
     } else {
       float s, c;
-      sincospif((float)half_turns(p, f), &s, &c);
+      cos_sin(p, f, &c, &s);
       ((float2*)table)[i] = make_float2(c, s);
     }
   }

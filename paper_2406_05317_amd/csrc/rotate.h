@@ -237,6 +237,19 @@ __device__ __forceinline__ double half_turns(int32_t position, float freq) {
   return r - 2.0 * rint(r * 0.5);
 }
 
+// Its cosine and sine in fp32.  They are taken of what it is from the nearest quarter turn, at most 1/4, which rounds to fp32 by 2^-27 or less and
+// near a zero of either by less: both are right to a few steps of their own size (rounded in half turns up to 1, by 2^-25, results were twice
+// as far from exact ones).
+__device__ __forceinline__ void cos_sin(int32_t position, float freq, float* c, float* s) {
+  const double h = half_turns(position, freq), quarters = rint(2.0 * h);
+  const int32_t k = (int32_t)quarters;
+  float x, y;
+  sincospif((float)(h - 0.5 * quarters), &y, &x);
+  const float a = k & 1 ? -y : x, b = k & 1 ? x : y;
+  *c = k & 2 ? -a : a;
+  *s = k & 2 ? -b : b;
+}
+
 // sums over the P lanes of a row; in fp32 up to 16 lanes without a trip through the LDS crossbar
 template <int CTRL>
 __device__ __forceinline__ float beside(float x) {

@@ -16,7 +16,7 @@ __device__ __forceinline__ void fill_table(float2* table, const RotateView& rv, 
     const int32_t x = i / half, token = min(token0 + x, tokens - 1);
     const int32_t pos = positions ? positions[token] : token % t;
     float s, c;
-    sincospif((float)half_turns(pos, rv.freqs[i - x * half]), &s, &c);
+    cos_sin(pos, rv.freqs[i - x * half], &c, &s);
     table[i] = make_float2(c, s);
   }
 }

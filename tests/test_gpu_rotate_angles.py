@@ -55,6 +55,31 @@ def test_cosines_and_sines_of_far_positions(adjacent):
         assert not bad.any(), (bad.sum().item(), (mine - want).abs().max().item() / U)
 
 
+@pytest.mark.parametrize("top", [100, 4096, 2 ** 31 - 1])
+def test_cosines_and_sines_to_steps_of_their_own_size(top):
+    """Relative to each value, those beside a zero among them.  The angle is counted from the nearest quarter turn, at most 1/4 of a half turn: its
+    rounding, u of it, moves the sine by at most u of the sine and the cosine by pi/4 tan(pi/4) u < u of the cosine.  The function's own error: 2
+    steps, 4 u where a step is largest.  One u more for the angle's 2^-52 in 64 bits: no value here is below 2^-20."""
+    n, d = 400, 128
+    g = torch.Generator().manual_seed(top % 1000)
+    pos = (torch.rand(n, generator=g, dtype=torch.float64) * top).long().int()
+    freqs = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float()
+    out = torch.empty(2, 1, 1, n, d, device="cuda")
+    rot = lb.Rotation(dtype=torch.float32, n_q_heads=1, n_kv_heads=1, head_dim=d, freqs=freqs.cuda())
+    x = torch.zeros(1, 1, n, d, device="cuda")
+    x[..., :d // 2] = 1.0
+    lb.lococo_rows_rotate(rot, x, None, out[0], None, pos.cuda())
+    v = torch.zeros_like(x)
+    pages = lb.Pages(dtype=torch.float32, n_q_heads=1, n_kv_heads=1, head_dim=d, page_rows=16, n_pages=n // 16)
+    lb.lococo_pages_append(pages, rot, x, v, v, out[1], torch.arange(n, **I32), pos.cuda())
+    angle = left_over(pos, freqs)
+    want = torch.cat((torch.cos(angle), torch.sin(angle)), -1)
+    live = want.abs() >= 2.0 ** -20
+    for got in out.cpu().double()[:, 0, 0]:
+        bad = live & ~((got - want).abs() <= 6 * U * want.abs())
+        assert not bad.any(), (bad.sum().item(), ((got - want).abs() / want.abs())[bad].max().item() / U)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("adjacent", [False, True])
 @pytest.mark.parametrize("least,low", [(0, -4), (30, 3)])
