@@ -226,26 +226,26 @@ struct Pairs {
 };
 inline PairKind pair_kind(int32_t r, int32_t adjacent) { return adjacent ? kAdjacent : r % 8 ? kHalves : kHalves4; }
 
-// The angle position * freq in half turns, whole turns left out: in [-1, 1], off by some 2^-53 at any position and at
+// The angle position * freq in half turns, whole turns left out: in [-1, 1] or little beyond, off by some 2^-53 at any position and at
 // frequencies up to 2^24.  The product has up to 55 bits and 1 / pi has no end, so both are sums of two numbers: what a product leaves over is
 // an fma.
 __device__ __forceinline__ double half_turns(int32_t position, float freq) {
   constexpr double kHi = 0.3183098861837907, kLo = -1.9678676675182486e-17;    // of 1 / pi
   const double p = position, f = freq, a = p * f, h = a * kHi;
-  const double l = fma(a, kHi, -h) + fma(a, kLo, fma(p, f, -a) * kHi);
-  const double r = h - 2.0 * rint(h * 0.5) + l;
-  return r - 2.0 * rint(r * 0.5);
+  return h - 2.0 * rint(h * 0.5) + (fma(a, kHi, -h) + fma(a, kLo, fma(p, f, -a) * kHi));
 }
 
-// Its cosine and sine in fp32.  They are taken of what it is from the nearest quarter turn, at most 1/4, which rounds to fp32 by 2^-27 or less and
-// near a zero of either by less: both are right to a few steps of their own size (rounded in half turns up to 1, by 2^-25, results were twice
-// as far from exact ones).
+// Its cosine and sine in fp32, right to two steps of their own size.  They are taken of what it is from the nearest quarter turn, y in
+// [-pi / 4, pi / 4], which rounds to fp32 by 2^-25 or less and near a zero of either by less (rounded in half turns up to 1, by 2^-25 of them, results
+// were twice as far from exact ones).  sin y = y + y^3 P(y^2), cos y = 1 - y^2 / 2 + y^4 Q(y^2): P and Q of degree two by least maximum error, 0.06 u
+// and 0.002 u of the results.
 __device__ __forceinline__ void cos_sin(int32_t position, float freq, float* c, float* s) {
   const double h = half_turns(position, freq), quarters = rint(2.0 * h);
   const int32_t k = (int32_t)quarters;
-  float x, y;
-  sincospif((float)(h - 0.5 * quarters), &y, &x);
-  const float a = k & 1 ? -y : x, b = k & 1 ? x : y;
+  const float y = (float)((h - 0.5 * quarters) * 3.141592653589793), z = y * y;
+  const float si = fmaf(y * z, fmaf(z, fmaf(z, -0.00019517137843649834f, 0.008332177065312862f), -0.16666655242443085f), y);
+  const float co = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.4438271793769673e-05f, -0.0013887366512790322f), 0.04166664555668831f), -0.5f), 1.f);
+  const float a = k & 1 ? -si : co, b = k & 1 ? co : si;
   *c = k & 2 ? -a : a;
   *s = k & 2 ? -b : b;
 }
