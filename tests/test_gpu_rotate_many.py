@@ -1,0 +1,112 @@
+"""Rotated rows in numbers that fill the device: workgroups of many positions, heads in turn, several tiles of positions one after the other.
+(test_rotate_layouts_cpu.py holds the cases to those layouts.)  Tolerances are those of test_gpu_rotate.py where nothing else is said."""
+import math
+
+import pytest
+import torch
+
+import pages_util as pu
+import rotate_util as ru
+import test_gpu_rotate as small
+from paper_2406_05317_amd import binding as lb
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+# b, t, Hq, Hkv, d, r, adjacent, norm, weights: a second block of heads, odd numbers of them, a last tile that is not full
+FORWARDS = [(1, 2907, 17, 3, 128, 128, False, True, "shared"), (3, 1931, 19, 33, 64, 32, True, True, "heads"),
+            (1, 2901, 18, 16, 96, 90, False, False, "none"), (2, 703, 35, 1, 256, 256, True, True, "shared"),
+            (1, 1403, 33, 17, 200, 96, False, True, "heads")]
+# the same and page_rows
+APPENDS = [(2, 1203, 34, 17, 128, 128, False, True, "shared", 64), (1, 4003, 19, 19, 64, 32, True, True, "heads", 32),
+           (3, 941, 18, 18, 96, 90, False, False, "none", 16), (1, 701, 40, 20, 256, 256, False, True, "heads", 128)]
+# weights' gradients: more tiles than workgroups to a block of heads, the last workgroup with fewer of them
+BACKWARDS = [(1, 8521, 64, 64, 64, 64, False, True, "shared"), (1, 617, 64, 64, 128, 64, True, True, "heads"), (2, 337, 100, 20, 96, 90, False, True, "heads")]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", range(len(FORWARDS)))
+def test_forward_of_many_rows(dtype, kind):
+    b, t, Hq, Hkv, d, r, adjacent, norm, weights = FORWARDS[kind]
+    print(dtype, FORWARDS[kind], flush=True)
+    rot, rows, pos, ws, _ = small.make(kind + 400, dtype, *FORWARDS[kind], layout="tokens", far=1000000, nobody=0.1)
+    pos[-2] = -1
+    q, k = rows[:, :Hq], rows[:, Hq:]
+    wide = torch.full((b, t, Hq + Hkv, d + 8), 5.0, dtype=dtype, device="cuda")
+    qo, ko = wide[:, :, :Hq, :d].transpose(1, 2), wide[:, :, Hq:, :d].transpose(1, 2)
+    lb.lococo_rows_rotate(rot, q, k, qo, ko, pos)
+    assert torch.equal(wide[..., d:], torch.full_like(wide[..., d:], 5.0))
+    small.check_forward(rot, q, ws[0], pos, qo, adjacent, norm, 5.0)
+    small.check_forward(rot, k, ws[1], pos, ko, adjacent, norm, 5.0)
+    before, real = q.clone(), (pos.reshape(b, 1, t, 1) >= 0).expand_as(q)
+    lb.lococo_rows_rotate(rot, q, None, q, None, pos)
+    assert torch.equal(q, torch.where(real, qo, before))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", range(len(APPENDS)))
+def test_append_of_many_rows(dtype, kind):
+    """Codes and scales equal those of the 64-bit definition: every one."""
+    b, t, Hq, Hkv, d, r, adjacent, norm, weights, R = APPENDS[kind]
+    print(dtype, APPENDS[kind], flush=True)
+    rot, rows, pos, ws, g = small.make(kind + 500, dtype, b, t, Hq, Hkv, d, r, adjacent, norm, weights, layout="tokens", far=200000, extra=Hkv)
+    q, k, v = rows[:, :Hq], rows[:, Hq:Hq + Hkv], rows[:, Hq + Hkv:]
+    slots, n_pages = small.placed(g, b, t, R)
+    pages = lb.Pages(dtype=dtype, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, page_rows=R, n_pages=n_pages)
+    marks = (pages.k_codes, pages.k_scales, pages.v_codes, pages.v_scales)
+    for x in marks:
+        x.fill_(0x5a)
+    pos[::11] = -1
+    pos[-2] = -1
+    slots[pos.cpu() < 0] = -1
+    slots[3::29] = n_pages * R
+    qo = torch.full((b, Hq, t, d), 5.0, dtype=dtype, device="cuda")
+    lb.lococo_pages_append(pages, rot, q, k, v, qo, slots.cuda(), pos)
+    small.check_forward(rot, q, ws[0], pos, qo, adjacent, norm, 5.0)
+    keys = ru.forward(k.cpu(), None if ws[1] is None else ws[1].cpu(), ru.angles(pos.cpu(), rot.freqs.cpu()).reshape(b, t, -1), r, adjacent, norm,
+                      small.EPS)
+    on = (slots >= 0) & (slots < n_pages * R)
+    page, row = (slots[on] // R).long(), (slots[on] % R).long()
+    got = [x.cpu() for x in marks]
+    want = [torch.full_like(x, 0x5a) for x in got]
+    for x, codes, scales in ((keys, *want[:2]), (v.cpu().double(), *want[2:])):
+        for h in range(Hkv):
+            code, scale = pu.four_bits(x[:, h].reshape(b * t, d)[on])
+            codes[page, h, row] = code[..., 0::2] | (code[..., 1::2] << 4)
+            scales[page, h, :, row] = scale
+    for i, (x, y) in enumerate(zip(got, want)):
+        assert torch.equal(x, y), (i, (x != y).sum().item(), (x != y).nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("kind", range(len(BACKWARDS)))
+def test_weights_gradients_over_several_tiles(kind):
+    """Upstream gradients that go with the rows, so that a weight's gradient is about its number of rows, and what a tile contributes is far above
+    the tolerance.  Of a term G xhat: G is off by 10 u (|g_a| + |g_b|), xhat by (d / 2 + 5) u, their product by u; of eight terms in fp32, parts
+    rounded to fp32 and the last rounding: 8 + 1 + 1 u.  Sums beyond that in 64 bits.  Together (d / 2 + 26) u sum (|g_a| + |g_b|) |xhat|."""
+    b, t, Hq, Hkv, d, r, adjacent, norm, weights = BACKWARDS[kind]
+    rot, rows, pos, ws, g = small.make(kind + 600, torch.bfloat16, *BACKWARDS[kind], far=100000, nobody=0.02)
+    real = (pos >= 0).reshape(b, 1, t, 1)
+    angle = small.angle_of(rot, pos, b, t).cuda()
+    q, k = rows[:, :Hq], rows[:, Hq:]
+    gy, hats = [], []
+    for x in (q, k):
+        hat = ru.normed(x, None, True, small.EPS)[1]
+        mixed = hat + 0.5 * torch.randn(x.shape, device="cuda")
+        gy.append(ru.turn(mixed, angle, r, adjacent).float())
+        hats.append(hat)
+    gx = [torch.full_like(x, math.nan) for x in gy]
+    gw = [torch.full(w.shape, 2.0, device="cuda") for w in ws]
+    work = lb.rotate_workspace(rot, b * t)
+    work.fill_(255)
+    lb.lococo_rows_rotate_backward(rot, q, k, pos, *gy, *gx, *gw, work)
+    rows_of_tile = 256 // max(1, 1 << (d // 8 - 1).bit_length())
+    for w, y, hat, got, dx in zip(ws, gy, hats, gw, gx):
+        y = y.double() * real
+        G = ru.turn(y, angle, r, adjacent, back=True)
+        dims = (0, 1, 2) if w.dim() == 1 else (0, 2)
+        want, size = (G * hat).sum(dims), (ru.reach(y, r, adjacent) * hat.abs()).sum(dims)
+        tol = (d / 2 + 26) * U * size + 2 * U * 2.0
+        assert ((got.double() - 2.0 - want).abs() <= tol).all(), ((got.double() - 2.0 - want).abs() / tol).max().item()
+        # a tile's share is not lost in it
+        assert (want.abs() * rows_of_tile / (b * t) > 4 * tol).all()
+        assert torch.isfinite(dx).all() and not dx[(~real).expand_as(dx)].any()
