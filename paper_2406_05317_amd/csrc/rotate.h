@@ -307,6 +307,7 @@ struct RotateBackArgs {
   int32_t tokens, t;
   int32_t blocks[2];
   int32_t chunks, tiles;                       // workgroups to a block of heads, tiles of positions to a workgroup
+  int32_t stretch;                             // tiles whose part of d_w a lane adds up in fp32
   float* parts;                                // [block][chunk][d]
 };
 

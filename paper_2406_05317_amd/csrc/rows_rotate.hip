@@ -114,13 +114,17 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
 
 // The way back: g_n = the upstream gradient turned the other way; with xhat = x * one, one = 1 / sqrt(mean(x^2) + eps),
 //   d_w += g_n xhat (over all rows),  d_x = one * (w g_n - xhat mean(w g_n xhat)).
-// Both means are sums over the row taken side by side.  A workgroup adds up its rows' part of d_w in registers, once over its rows in LDS at
-// the end, and leaves it for rows_rotate_weights_k: no atomics, the same bits every time.  Bound by memory: 16384 positions of 40 heads, 839 MB in
-// 167 us (5.0 TB/s), the weights' parts 8 more; with half as many workgroups 171, with a quarter 188.
+// Both means are sums over the row taken side by side.  A workgroup adds up its rows' part of d_w, once over its rows in LDS at the end, and
+// leaves it for rows_rotate_weights_k: no atomics, the same bits every time.  d_w is a sum over all rows of all heads: in fp32 over the eight
+// or fewer that a lane has of one tile (of eight tiles, where it has one of each), beyond them in 64 bits, a workgroup's part rounded to fp32.
+// In fp32 throughout it was twice as far from the exact sum.  Bound by memory: 16384 positions of 40 heads, 839 MB in 167 us (5.0 TB/s), the
+// weights' parts 8 more; with half as many workgroups 171, with a quarter 188.
+constexpr int kBackRows = 8;                   // rows whose part of d_w a lane adds up in fp32
+
 template <typename T, int KIND>
-__global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackArgs a) {
+__global__ __launch_bounds__(kRotateThreads, 4) void rows_rotate_back_k(RotateBackArgs a) {
   __shared__ float2 table[kRotateTable];
-  __shared__ float gws[kRotateThreads * 8];
+  __shared__ double gws[kRotateThreads * 8];
   const RotateView& rv = a.rv;
   const int32_t blk = blockIdx.x / a.chunks, chunk = blockIdx.x - blk * a.chunks;
   const int part = blk >= a.blocks[0];
@@ -132,8 +136,21 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
   const T* weights = (const T*)rv.w[part];
   float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
   if (weights && !banks && in) pr.load(weights, wa, wb);
+  // a lane's sums in 64 bits lie in LDS: in registers they would cost a fourth of the waves
+  double* mine = gws + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mine[i * kRotateThreads] = 0.0;
   float gwa[4] = {0.f, 0.f, 0.f, 0.f}, gwb[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&] {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mine[i * kRotateThreads] += gwa[i];
+      mine[(4 + i) * kRotateThreads] += gwb[i];
+      gwa[i] = gwb[i] = 0.f;
+    }
+  };
   for (int32_t k = 0; k < a.tiles; ++k) {
+    if (k && k % a.stretch == 0) add();
     const int64_t first = ((int64_t)chunk * a.tiles + k) << lt;
     if (first >= a.tokens) break;              // the same for all lanes
     const int32_t token0 = (int32_t)first, token = token0 + sub;
@@ -200,27 +217,32 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_back_k(RotateBackA
     }
   }
   if (!a.gw[part]) return;
+  add();
+  double dw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) dw[i] = mine[i * kRotateThreads];
+  __syncthreads();
   if (in)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      gws[grp * rv.d + pr.first(i)] = gwa[i];
-      gws[grp * rv.d + pr.second(i)] = gwb[i];
+      gws[grp * rv.d + pr.first(i)] = dw[i];
+      gws[grp * rv.d + pr.second(i)] = dw[4 + i];
     }
   __syncthreads();
   for (int32_t c = threadIdx.x; c < rv.d; c += kRotateThreads) {
-    float sum = 0.f;
+    double sum = 0.0;
     for (int32_t k = 0; k < kRotateThreads >> lp; ++k) sum += gws[k * rv.d + c];
-    a.parts[((int64_t)blk * a.chunks + chunk) * rv.d + c] = sum;
+    a.parts[((int64_t)blk * a.chunks + chunk) * rv.d + c] = (float)sum;
   }
 }
 
-// The parts of a weight's gradient to one, in a fixed order, and onto what is there: a workgroup to 16 columns of a bank of weights, lanes of
-// four columns, eight rows on their way at once.
+// The parts of a weight's gradient to one, in 64 bits and a fixed order, and onto what is there: a workgroup to 16 columns of a bank of
+// weights, lanes of four columns, eight rows on their way at once.
 constexpr int kWeightThreads = 1024, kWeightCols = 16, kWeightRows = 8;
 
 __global__ __launch_bounds__(kWeightThreads) void rows_rotate_weights_k(RotateBackArgs a) {
   constexpr int LANES = kWeightCols / 4, SIDE = kWeightThreads / LANES;
-  __shared__ __align__(16) float sums[SIDE][kWeightCols];
+  __shared__ double sums[SIDE][kWeightCols];
   const RotateView& rv = a.rv;
   // banks: q's (one, or one a head), then k's
   const int32_t cols = (rv.d + kWeightCols - 1) / kWeightCols, bank = blockIdx.x / cols, c0 = (blockIdx.x - bank * cols) * kWeightCols;
@@ -231,7 +253,7 @@ __global__ __launch_bounds__(kWeightThreads) void rows_rotate_weights_k(RotateBa
   const int32_t first = (part ? a.blocks[0] : 0) + (rv.ws[part] ? head : 0), rows = (rv.ws[part] ? 1 : a.blocks[part]) * a.chunks;
   const int32_t k = threadIdx.x / LANES, c = 4 * (threadIdx.x % LANES);
   const float* at = a.parts + (int64_t)first * a.chunks * rv.d + c0 + c;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
   if (c0 + c < rv.d)
     for (int32_t i = k; i < rows; i += kWeightRows * SIDE) {
       float x[kWeightRows][4];
@@ -242,20 +264,20 @@ __global__ __launch_bounds__(kWeightThreads) void rows_rotate_weights_k(RotateBa
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += i + j * SIDE < rows ? x[j][e] : 0.f;
     }
-  write4(&sums[k][c], sum);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sums[k][c + e] = sum[e];
   for (int32_t n = SIDE / 2; n >= 1; n /= 2) {
     __syncthreads();
-    if (k < n) {
-      float other[4];
-      read4(&sums[k + n][c], other);
+    if (k < n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += other[e];
-      write4(&sums[k][c], sum);
-    }
+      for (int e = 0; e < 4; ++e) sums[k][c + e] = sum[e] += sums[k + n][c + e];
   }
   if (k == 0 && c0 + c < rv.d)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) a.gw[part][head * rv.ws[part] + c0 + c + e] += sum[e];
+    for (int e = 0; e < 4; ++e) {
+      float* gw = a.gw[part] + head * rv.ws[part] + c0 + c + e;
+      *gw = (float)(*gw + sum[e]);
+    }
 }
 
 struct BackPlan { RotateShape sh; int32_t blocks[2], chunks, tiles; };
@@ -264,7 +286,7 @@ BackPlan back_plan(const RotateView& rv, int32_t tokens) {
   p.sh.lp = lanes_log(rv.d);
   p.sh.lt = 8 - p.sh.lp;                       // positions alone: a workgroup's rows of a head lie side by side
   const bool banks = rv.ws[0] || rv.ws[1];
-  p.sh.hb = banks ? 1 : 8;
+  p.sh.hb = banks ? 1 : kBackRows;
   int64_t blocks = 0;
   for (int i = 0; i < 2; ++i) blocks += p.blocks[i] = (rv.heads[i] + p.sh.hb - 1) / p.sh.hb;
   const int64_t tiles = std::max<int64_t>(((int64_t)tokens + (1 << p.sh.lt) - 1) >> p.sh.lt, 1);
@@ -340,6 +362,7 @@ hipError_t launch_rows_rotate_backward(int dtype, RotateBackArgs a, void* worksp
   a.blocks[1] = p.blocks[1];
   a.chunks = p.chunks;
   a.tiles = p.tiles;
+  a.stretch = kBackRows / p.sh.hb;
   a.parts = (float*)workspace;
   const unsigned grid = (unsigned)((p.blocks[0] + p.blocks[1]) * p.chunks);
   switch (pair_kind(a.rv.r, a.rv.adjacent)) {

@@ -110,3 +110,28 @@ def test_weights_gradients_over_several_tiles(kind):
         # a tile's share is not lost in it
         assert (want.abs() * rows_of_tile / (b * t) > 4 * tol).all()
         assert torch.isfinite(dx).all() and not dx[(~real).expand_as(dx)].any()
+
+
+@pytest.mark.parametrize("weights", ["shared", "heads"])
+def test_weights_gradients_add_up_in_64_bits(weights):
+    """Rows of ones with signs (their root is one, to within a step that all share), gradients that cancel from one stretch of tiles to the one after
+    the next: 2^25, small whole numbers, -2^25.  What lies between is 22 bits below and is all that stays: whole numbers below 2^24, off by 2 u.
+    A workgroup has 24 tiles in turn, a head's weights its own workgroups: stretches of eight; or three tiles, of eight heads: stretches of one."""
+    cu = torch.cuda.get_device_properties(0).multi_processor_count
+    H, d, per = 64, 128, 16
+    t = 24 * per * (16 * cu // (2 * H))
+    g = torch.Generator(device="cuda").manual_seed(700)
+    x = (torch.randint(0, 2, (1, 2 * H, t, d), generator=g, device="cuda") * 2 - 1).float()
+    w = torch.ones((H, d) if weights == "heads" else (d,), device="cuda")
+    rot = lb.Rotation(dtype=torch.float32, n_q_heads=H, n_kv_heads=H, head_dim=d, norm=True, norm_eps=1e-12, q_weight=w, k_weight=w.clone())
+    v = torch.randint(1, 6, (1, 2 * H, t, d), generator=g, device="cuda").float()
+    third = torch.arange(t, device="cuda") // (per * (8 if weights == "heads" else 1)) % 3
+    v[:, :, third == 0], v[:, :, third == 2] = 2.0 ** 25, -(2.0 ** 25)
+    gy = v * x
+    q, k, gq, gk = x[:, :H], x[:, H:], gy[:, :H].contiguous(), gy[:, H:].contiguous()
+    gw = [torch.zeros_like(w) for _ in range(2)]
+    lb.lococo_rows_rotate_backward(rot, q, k, None, gq, gk, gq, gk, *gw, lb.rotate_workspace(rot, t))
+    small_ones = v[:, :, third == 1].double()
+    for got, part in zip(gw, (small_ones[:, :H], small_ones[:, H:])):
+        want = part.sum((0, 2) if weights == "heads" else (0, 1, 2))
+        assert ((got.double() - want).abs() <= 2 * U * want).all()
