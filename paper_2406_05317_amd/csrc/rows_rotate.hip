@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
   const bool active = pr.in() && token < a.tokens && (!a.positions || a.positions[min(token, a.tokens - 1)] >= 0);
   float c[4], s[4];
   read_table(table, pr, sub, c, s);
-  // times the weights: y_a = one (x_a ca - x_b sb), y_b = one (x_b cb + x_a sa)
+  // times the weights: with xhat = one x, which is not large, y_a = xhat_a ca - xhat_b sb, y_b = xhat_b cb + xhat_a sa
   const T* weights = (const T*)rv.w[part];
   const bool banks = weights && rv.ws[part];
   float ca[4], cb[4], sa[4], sb[4];
@@ -84,28 +84,12 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
     for (int k = 0; k < kAhead; ++k) {
       if (h + k * step >= h1) break;
       if (banks) weigh(h + k * step);
-      float one = 1.f;
-      if (rv.norm) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum = fmaf(xa[k][i], xa[k][i], fmaf(xb[k][i], xb[k][i], sum));
-        sum = row_sum(sum, lp);
-        one = rsqrtf(sum * (1.f / (float)rv.d) + rv.eps);
-        if (sum == INFINITY) {
-          const float x = one_of_large(xa[k], xb[k], lp, rv);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            xa[k][i] *= x;
-            xb[k][i] *= x;
-          }
-          one = 1.f;
-        }
-      }
+      const float one = rv.norm ? one_over_root(xa[k], xb[k], lp, rv) : 1.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float ya = fmaf(xa[k][i], ca[i], -xb[k][i] * sb[i]), yb = fmaf(xb[k][i], cb[i], xa[k][i] * sa[i]);
-        xa[k][i] = one * ya;
-        xb[k][i] = one * yb;
+        const float na = one * xa[k][i], nb = one * xb[k][i];
+        xa[k][i] = fmaf(na, ca[i], -nb * sb[i]);
+        xb[k][i] = fmaf(nb, cb[i], na * sa[i]);
       }
       if (active) pr.store(out + (h + k * step) * a.out[part].sh, xa[k], xb[k]);
     }
@@ -196,7 +180,7 @@ __global__ __launch_bounds__(kRotateThreads, 4) void rows_rotate_back_k(RotateBa
           sq = row_sum(sq, lp);
           dot = row_sum(dot, lp);
           float one = rsqrtf(sq * (1.f / (float)rv.d) + rv.eps), mean = one * dot * (1.f / (float)rv.d);
-          if (sq == INFINITY) {                // so may the other sum be
+          if (!(sq < INFINITY && fabsf(dot) < INFINITY)) {
             one = one_of_large(xa[j], xb[j], lp, rv);
             dot = 0.f;
 #pragma unroll

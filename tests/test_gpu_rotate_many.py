@@ -135,3 +135,24 @@ def test_weights_gradients_add_up_in_64_bits(weights):
     for got, part in zip(gw, (small_ones[:, :H], small_ones[:, H:])):
         want = part.sum((0, 2) if weights == "heads" else (0, 1, 2))
         assert ((got.double() - want).abs() <= 2 * U * want).all()
+
+
+def test_products_beyond_fp32():
+    """Results and gradients that fp32 holds, of rows whose products with weights or gradients it does not: 1e18 times 1e21."""
+    b, t, H, d = 1, 40, 2, 128
+    g = torch.Generator().manual_seed(710)
+    x = (1e18 * torch.randn(b, 2 * H, t, d, generator=g)).cuda()
+    freqs = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().cuda()
+    for size_w, size_g in ((1e21, 1.0), (1.0, 1e22)):
+        w = (size_w * (1 + 0.3 * torch.randn(d, generator=g))).cuda()
+        rot = lb.Rotation(dtype=torch.float32, n_q_heads=H, n_kv_heads=H, head_dim=d, freqs=freqs, norm=True, norm_eps=1e-5, q_weight=w, k_weight=w)
+        q, k = x[:, :H], x[:, H:]
+        outs = [torch.full_like(q, 5.0) for _ in range(2)]
+        lb.lococo_rows_rotate(rot, q, k, *outs)
+        gy = [(size_g * torch.randn(q.shape, generator=g)).cuda() for _ in range(2)]
+        gx = [torch.empty_like(y) for y in gy]
+        gw = [torch.zeros(d, device="cuda") for _ in range(2)]
+        lb.lococo_rows_rotate_backward(rot, q, k, None, *gy, *gx, *gw, lb.rotate_workspace(rot, t))
+        for rows, out, y, dx, dw in zip((q, k), outs, gy, gx, gw):
+            small.check_forward(rot, rows, w, None, out, False, True, 5.0)
+            small.check_backward(rot, rows, w, None, y, dx, dw, False, True)
