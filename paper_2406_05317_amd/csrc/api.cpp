@@ -2145,7 +2145,6 @@ lococo_status lococo_pages_attn_tree_workspace_bytes(const lococo_pages* pages, 
   if (!out) return fail(LOCOCO_EINVAL, "out is NULL");
   if ((st = check_pages(pages, true)) || (st = check_requests(pages, requests, false))) return st;
   const PagesAttnArgs a = pages_attn_args(pages, requests);
-  if (!pages_attn_tree_fits(pages->dtype, a)) return fail(LOCOCO_EUNSUPPORTED, "more query rows than one launch takes");
   *out = align_up(pages_attn_tree_workspace_bytes(pages->dtype, a), 256);
   return LOCOCO_OK;
 }
@@ -2165,7 +2164,6 @@ lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const lococo_req
   a.q = rows_view(q, rows_per_batch);
   a.o = rows_view(o, rows_per_batch);
   a.max_held = (int32_t)std::min<int64_t>(a.max_held, (int64_t)a.table_pages * pages->page_rows);
-  if (!pages_attn_tree_fits(pages->dtype, a)) return fail(LOCOCO_EUNSUPPORTED, "more query rows than one launch takes");
   const size_t need = align_up(pages_attn_tree_workspace_bytes(pages->dtype, a), 256);
   if (need && (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < need))
     return fail(LOCOCO_EWORKSPACE, "attention under masks needs %zu bytes of workspace, 256-byte aligned (got %zu)", need,

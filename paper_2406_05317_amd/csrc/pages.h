@@ -110,8 +110,7 @@ hipError_t launch_pages_move(const PagesMoveArgs& a, hipStream_t s);
 bool pages_attn_fits(int dtype, const PagesAttnArgs& a);     // a launch takes the work
 size_t pages_attn_workspace_bytes(int dtype, const PagesAttnArgs& a);
 hipError_t launch_pages_attn(int dtype, const PagesAttnArgs& a, void* workspace, hipStream_t s);
-// ---- pages_attn_tree.hip: the same sizes, a mask of `words` words for each of the call's rows
-bool pages_attn_tree_fits(int dtype, const PagesAttnArgs& a);
+// ---- pages_attn_tree.hip: the same sizes (those that pages_attn_fits), a mask of `words` words for each of the call's rows
 size_t pages_attn_tree_workspace_bytes(int dtype, const PagesAttnArgs& a);
 hipError_t launch_pages_attn_tree(int dtype, const PagesAttnArgs& a, const uint32_t* masks, int32_t words, void* workspace, hipStream_t s);
 

@@ -241,7 +241,7 @@ TreePlan tree_plan(int dtype, const PagesAttnArgs& a) {
   p.groups = (tiles * a.pg.Hkv + kParts + 63) / 64 * 64;
   // what the requests would cost if all were as long as the longest: steps of the waves that are resident
   const int64_t steps = tiles * a.pg.Hkv * (((int64_t)a.max_held + kTileKeys - 1) / kTileKeys) / (2 * kTileWaves * (int64_t)cu_count());
-  p.dealt = a.max_held > kAlone * kTileKeys && steps >= 16;
+  p.dealt = a.max_held > kAlone * kTileKeys && steps >= 16 && p.groups * kTileThreads <= kLaunchThreads;
   p.dealt_bytes = (sizeof(Dealt) + (size_t)p.groups * sizeof(Item) + 255) / 256 * 256;
   return p;
 }
@@ -275,10 +275,6 @@ hipError_t launch_tiles(const PagesAttnArgs& a, const TreeMasks& tm, const TreeP
 }
 
 }  // namespace
-
-bool pages_attn_tree_fits(int dtype, const PagesAttnArgs& a) {
-  return !tile_fits(a.pg.d) || tree_plan(dtype, a).groups * kTileThreads <= kLaunchThreads;
-}
 
 size_t pages_attn_tree_workspace_bytes(int dtype, const PagesAttnArgs& a) {
   if (!tile_fits(a.pg.d)) return 0;

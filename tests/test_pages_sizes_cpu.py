@@ -1,0 +1,28 @@
+"""Which sizes attention over pages takes under masks, and what workspace is allocated for it (CPU: nothing is run)."""
+import ctypes as C
+
+import pytest
+
+from paper_2406_05317_amd import binding as lb
+from test_pages_cpu import pages, requests
+
+
+def sizes(p, r):
+    L, out = lb.lib(), C.c_size_t(0)
+    a = L.lococo_pages_workspace_bytes(C.byref(p), C.byref(r), C.byref(out)), out.value
+    return a, (L.lococo_pages_attn_tree_workspace_bytes(C.byref(p), C.byref(r), C.byref(out)), out.value)
+
+
+@pytest.mark.parametrize("over,n,new", [
+    (dict(n_q_heads=4095, n_kv_heads=4095), 4096, 16),                       # a tile to a request: 2^24 - 4096 workgroups
+    (dict(n_q_heads=32, n_kv_heads=32), 1, 32 * (2 ** 19 - 2) + 31),         # 32 rows a workgroup, up to the launch's last one
+    (dict(head_dim=64, n_q_heads=32, n_kv_heads=32, dtype=lb.LOCOCO_F32), 1, 16 * (2 ** 19 - 2) + 15),
+    (dict(head_dim=96, n_q_heads=1, n_kv_heads=1), 1, 4 * (2 ** 24 - 1))])
+@pytest.mark.parametrize("held", [0, 300, 30000])
+def test_masks_take_the_sizes_that_causal_attention_takes(over, n, new, held):
+    p = pages(**over)
+    (a, _), (b, _) = sizes(p, requests(n=n, tokens=n * new, max_new=new, max_held=held))
+    assert a == b == lb.LOCOCO_OK
+    if n == 1:
+        (a, _), (b, _) = sizes(p, requests(n=1, tokens=new + 1, max_new=new + 1, max_held=held))
+        assert a == b == lb.LOCOCO_EUNSUPPORTED
