@@ -63,7 +63,7 @@ class Requests:
         o.masked_fill_((slots < 0).view(o.shape[0], 1, o.shape[2], 1), 0)
 
     def workspace(self, tokens: int, max_new: int):
-        return lb.pages_workspace(self.pages, self.n, tokens, max_new, self.most)
+        return lb.pages_workspace(self.pages, self.n, tokens, max_new, self.most, trees=False)
 
 
 def compress(prompt_k, prompt_v, q, filters):

@@ -709,11 +709,13 @@ def workspace(cfg, L: int, B: int, history: bool = False, device="cuda") -> torc
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device) if n else None
 
 
-def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int) -> torch.Tensor | None:
-    """Allocate (through torch) the workspace of lococo_pages_attn and lococo_pages_attn_tree calls of these sizes (max_held may be larger
-    than theirs)."""
-    need = max(lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held),
-               lococo_pages_attn_tree_workspace_bytes(pages, n, tokens, max_new, max_held))
+def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int, trees: bool = True) -> torch.Tensor | None:
+    """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes (max_held may be larger than theirs) and, unless
+    `trees` is False, of lococo_pages_attn_tree calls, which may take 17 MB and 48 bytes a
+    tile of rows where the others take nothing."""
+    need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
+    if trees:
+        need = max(need, lococo_pages_attn_tree_workspace_bytes(pages, n, tokens, max_new, max_held))
     return torch.empty(need, dtype=torch.uint8, device=pages.device) if need else None
 
 

@@ -1,5 +1,6 @@
 """Which sizes attention over pages takes under masks, and what workspace is allocated for it (CPU: nothing is run)."""
 import ctypes as C
+import types
 
 import pytest
 
@@ -26,3 +27,18 @@ def test_masks_take_the_sizes_that_causal_attention_takes(over, n, new, held):
     if n == 1:
         (a, _), (b, _) = sizes(p, requests(n=1, tokens=new + 1, max_new=new + 1, max_held=held))
         assert a == b == lb.LOCOCO_EUNSUPPORTED
+
+
+def test_workspaces_without_trees_are_those_of_causal_attention():
+    """No more than lococo_pages_attn asks for: none for one prompt of 2000 rows, which its tiles fill the device with."""
+    p = pages(n_q_heads=32, n_kv_heads=8)
+    here = types.SimpleNamespace(ref=C.byref(p), device="cpu")
+    seen = set()
+    for n, new, held in ((1, 2000, 2000), (32, 64, 8192), (32, 1, 8192), (1, 1, 100), (1, 1, 100000), (7, 0, 500)):
+        (_, causal), (_, trees) = sizes(p, requests(n=n, tokens=n * new, max_new=new, max_held=held))
+        for need, kw in ((causal, dict(trees=False)), (max(causal, trees), {})):
+            ws = lb.pages_workspace(here, n, n * new, new, held, **kw)
+            assert (0 if ws is None else ws.numel()) == need
+        seen.add(causal < trees)
+    assert sizes(p, requests(n=1, tokens=2000, max_new=2000, max_held=2000))[0] == (lb.LOCOCO_OK, 0)
+    assert seen == {True, False}
