@@ -711,8 +711,7 @@ def workspace(cfg, L: int, B: int, history: bool = False, device="cuda") -> torc
 
 def pages_workspace(pages: Pages, n: int, tokens: int, max_new: int, max_held: int, trees: bool = True) -> torch.Tensor | None:
     """Allocate (through torch) the workspace of lococo_pages_attn calls of these sizes (max_held may be larger than theirs) and, unless
-    `trees` is False, of lococo_pages_attn_tree calls, which may take 17 MB and 48 bytes a
-    tile of rows where the others take nothing."""
+    `trees` is False, of lococo_pages_attn_tree calls, which may take 17 MB and 48 bytes a tile of rows where the others take nothing."""
     need = lococo_pages_workspace_bytes(pages, n, tokens, max_new, max_held)
     if trees:
         need = max(need, lococo_pages_attn_tree_workspace_bytes(pages, n, tokens, max_new, max_held))

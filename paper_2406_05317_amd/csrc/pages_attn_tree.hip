@@ -103,7 +103,8 @@ __global__ __launch_bounds__(kDealThreads) void pages_tree_deal_k(DealtArgs g) {
   }
   scan(work, &all_work, part);
   const int64_t even = ((int64_t)all_work * a.pg.Hkv + kParts * kTileWaves - 1) / (kParts * kTileWaves);
-  const int32_t per = kTileWaves * (all_work < kPagesCap ? (int32_t)max(even, (int64_t)kLeastSteps) : kNoParts);      // steps of a part
+  // steps of a part
+  const int32_t per = kTileWaves * (all_work < kPagesCap ? (int32_t)min(max(even, (int64_t)kLeastSteps), (int64_t)kNoParts) : kNoParts);
   auto parts_of = [&](const Request& r) { return (r.steps + per - 1) / per; };
   int32_t n_long = 0, n_alone = 0, n_kept = 0, n_joins = 0, all_long, all_alone, all_kept, all_joins;
   for (int i = i0; i < i1; ++i) {
