@@ -554,9 +554,11 @@ LOCOCO_API lococo_status lococo_rows_rotate_backward(const lococo_rotation* rot,
 
 /* A turn's new rows into the pages as a projection leaves them: q_out = q normed and turned, k normed and turned and v to 4 bits at
  * slots[i]: lococo_rows_rotate and lococo_pages_store in one pass.  A slot outside the pages leaves its row of k and v out, a negative
- * position its row of q_out as it is.  slots, positions: device [tokens], as lococo_pages_plan or lococo_pages_tree leaves them; two
- * rows of a call must not share a slot.  Norm and rotation of k are in 64 bits: its codes are those nearest to the exact values, where
- * lococo_pages_store would take those nearest to rounded ones.  rot and pages describe the same rows (type, heads, head_dim).  q_out may be q. */
+ * position its row of q_out as it is.  A row of nobody that has a slot all the same (lococo_pages_tree can leave such rows) has its k
+ * turned by that negative number and stored: no mask should name it, and it is not to be kept.  slots, positions: device [tokens], as
+ * lococo_pages_plan or lococo_pages_tree leaves them; two rows of a call must not share a slot.  Norm and rotation of k are in 64 bits:
+ * its codes are those nearest to the exact values, where lococo_pages_store would take those nearest to rounded ones.  rot and pages
+ * describe the same rows (type, heads, head_dim).  q_out may be q. */
 LOCOCO_API lococo_status lococo_pages_append(const lococo_pages* pages, const lococo_rotation* rot, const lococo_tensor* q,
                                              const lococo_tensor* k, const lococo_tensor* v, const lococo_tensor* q_out,
                                              int32_t rows_per_batch, int32_t tokens, const int32_t* slots, const int32_t* positions,
@@ -580,7 +582,8 @@ LOCOCO_API lococo_status lococo_pages_append(const lococo_pages* pages, const lo
  * Numbers that are no earlier row count as -1.  A row stands as many positions behind bases[i] as it has ancestors (bases NULL: behind
  * held - new, so that a root's position is that of the request's first new row), and its mask holds its ancestors and itself: bit
  * j % 32 of word j / 32 of the row's mask_words words (1 .. 8) is new row j.  Of a request with more than 32 * mask_words new rows
- * those behind get position -1 and an empty mask, and so do rows that no request has.
+ * those behind get position -1 and an empty mask, and so do all rows of a request with a negative base and rows that no request has.
+ * A row at position -1 is not to be kept: what lococo_pages_append stores for it is a key of no position.
  *   out  masks [tokens][mask_words], positions [tokens] */
 LOCOCO_API lococo_status lococo_pages_tree(int32_t n, int32_t tokens, const int32_t* starts, const int32_t* held,
                                            const int32_t* bases, const int32_t* parents, int32_t mask_words, uint32_t* masks,
@@ -599,7 +602,8 @@ LOCOCO_API lococo_status lococo_pages_attn_tree(const lococo_pages* pages, const
                                                 int32_t mask_words, void* workspace, size_t ws_bytes, void* stream);
 
 /* The new rows whose number in kept [tokens] is not 0 stay, in their order: the first of a request's takes the slot of its first new
- * row, and so on.  slots: the plan's.  A request whose first new row has no slot was refused: it keeps what it held.
+ * row, and so on.  slots: the plan's.  A request whose first new row has no slot was refused: it keeps what it held.  Rows that
+ * lococo_pages_tree has left at position -1 must not be marked.
  *   in      tables [n][table_pages], starts [n + 1], held [n] (the plan's held_after), slots, kept [tokens], ends [2] (ends_after)
  *   in out  ring [n_pages]: pages that no row is left in go behind its last free one, request by request
  *   out     held_after [n], ends_after [2], sources, targets [tokens]: the slots a kept row moves between, -1 for rows that do not
