@@ -309,7 +309,7 @@ __device__ __forceinline__ void load_v(ValueCodes<D>& v, const PagesView& pg, in
 }
 
 // A tile's work on the keys key_lo .. key_hi - 1: to o where that is all it sees, else as a part, rows from part_row on.  WAVES waves take 64
-// keys in turn and meet at the end; one alone writes from where the products left its results.  tid: threadIdx.x.
+// keys in turn and meet at the end; one alone, for which it is all, writes from where the products left its results.  tid: threadIdx.x.
 template <typename T, int D, int QB, bool TREE, int WAVES>
 __device__ __forceinline__ void attn_piece(const TileArgs& g, const TreeMasks& tm, const TileJob& job, int32_t kvh, int32_t key_lo, int32_t key_hi,
                                            bool whole_job, int64_t part_row, int tid) {
@@ -556,10 +556,6 @@ __device__ __forceinline__ void attn_piece(const TileArgs& g, const TreeMasks& t
       const float inv = sum[qb][0] == 0.f ? 0.f : 1.f / sum[qb][0];           // a row that sees nothing: zeros
       const int32_t token = job.first + x, ob = token < a.o.t ? 0 : token / a.o.t, ot = token - ob * a.o.t;
       T* out = (T*)a.o.p + ob * a.o.sb + (kvh * pg.group + row - x * pg.group) * a.o.sh + ot * a.o.st;
-      if (!whole_job && grp == 0) {
-        g.part_ml[2 * (part_row + r)] = ref[qb];
-        g.part_ml[2 * (part_row + r) + 1] = sum[qb][0];
-      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int col = COLS * (4 * grp + i), block = col / 32;
@@ -572,11 +568,7 @@ __device__ __forceinline__ void attn_piece(const TileArgs& g, const TreeMasks& t
           if (odd) o[qb][j][i] = NAN;
           z[j] = (T)(o[qb][j][i] * inv);
         }
-        if (!whole_job) {
-#pragma unroll
-          for (int j = 0; j < COLS; j += 4)
-            *(f4*)(g.part_o + (part_row + r) * D + col + j) = f4{o[qb][j][i], o[qb][j + 1][i], o[qb][j + 2][i], o[qb][j + 3][i]};
-        } else if constexpr (PARTS == 1) {
+        if constexpr (PARTS == 1) {
           *(typename Bytes<COLS * 2>::type*)(out + col) = *(typename Bytes<COLS * 2>::type*)z;
         } else {
 #pragma unroll
