@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "lococo_internal.h"
 
 namespace lococo {
@@ -94,6 +96,40 @@ constexpr int kPagesMaxHeadDim = 256;
 constexpr int kPagesMinRows = 16, kPagesMaxRows = 1024;
 constexpr int32_t kPagesCap = 0x3fffffff;     // rows of a call, slots, rows of a request: below
 constexpr int kPagesMaxTree = 256;            // new rows of a request that masks can name, a multiple of 32
+
+// ---- what their kernels share
+typedef __attribute__((ext_vector_type(4))) uint32_t w4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f4_any;          // fp32 rows begin at any float
+
+// sums of numbers >= 0 cut off at kPagesCap
+__device__ __forceinline__ int32_t add_cap(int32_t x, int32_t y) { return min(x + y, kPagesCap); }
+
+// a head's row of a call's token
+template <typename T>
+__device__ __forceinline__ const T* row_at(const RowsView& r, int32_t token, int32_t head) {
+  const int32_t b = token < r.t ? 0 : token / r.t, t = token - b * r.t;
+  return (const T*)r.p + b * r.sb + head * r.sh + t * r.st;
+}
+
+// eight values of a row: bf16 rows begin at multiples of 16 bytes
+template <typename T>
+__device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
+  if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f4_any v = *(const f4_any*)(p + 4 * i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
+    }
+  } else {
+    const w4 v = *(const w4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  }
+}
 
 // ---- pages.hip
 hipError_t launch_pages_plan(const PagesPlanArgs& a, hipStream_t s);

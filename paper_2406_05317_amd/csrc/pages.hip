@@ -2,15 +2,11 @@
 #include "pages.h"
 #include "pages_codes.h"
 
-#include <type_traits>
-
 namespace lococo {
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;      // fp32 rows begin at any float
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Plan.  Three running sums over the requests give every row's place: of the new rows (where a request's rows begin in the call), of
@@ -21,8 +17,6 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;      //
 // Sums saturate at kPagesCap (addition cut off at a bound is associative for numbers >= 0): lengths that make no sense stay sums that
 // refuse.  Bound by the launch and some three round trips to memory: 5.3 us for 32 requests with a row each, 7.8 us for 512 with 52 K rows.
 constexpr int kPlanThreads = 256;
-
-__device__ __forceinline__ int32_t add_cap(int32_t a, int32_t b) { return min(a + b, kPagesCap); }
 
 // exclusive running sums of two numbers a thread over the workgroup; the totals in *t0, *t1
 __device__ __forceinline__ void scan_two(int32_t& x0, int32_t& x1, int32_t* t0, int32_t* t1, int32_t (*part)[2]) {
@@ -177,31 +171,6 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_k(PagesPlanArgs a) {
 constexpr int kRowThreads = 256;
 
 template <typename T>
-__device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
-  if constexpr (std::is_same<T, float>::value) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f32x4_any v = *(const f32x4_any*)(p + 4 * i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
-    }
-  } else {
-    const u32x4 v = *(const u32x4*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(v[i] << 16);
-      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ const T* row_of(const RowsView& r, int32_t token, int32_t head) {
-  const int32_t b = token < r.t ? 0 : token / r.t, t = token - b * r.t;
-  return (const T*)r.p + b * r.sb + head * r.sh + t * r.st;
-}
-
-template <typename T>
 __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsView k, RowsView v, int32_t tokens, const int32_t* slots) {
   const int32_t token = blockIdx.x * blockDim.y + threadIdx.y, c = threadIdx.x, head = blockIdx.y;
   if (token >= tokens) return;                   // the four lanes of a block leave together
@@ -209,8 +178,8 @@ __global__ __launch_bounds__(kRowThreads) void pages_store_k(PagesView pg, RowsV
   const int32_t page = slot >> pg.page_shift, row = slot & (pg.page_rows - 1);
   if (slot < 0 || page >= pg.n_pages) return;
   float x[2][8];
-  read8(row_of<T>(k, token, head) + 8 * c, x[0]);
-  read8(row_of<T>(v, token, head) + 8 * c, x[1]);
+  read8(row_at<T>(k, token, head) + 8 * c, x[0]);
+  read8(row_at<T>(v, token, head) + 8 * c, x[1]);
   const int64_t at = (int64_t)page * pg.Hkv + head;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -239,19 +208,19 @@ __global__ __launch_bounds__(kRowThreads) void pages_load_k(PagesView pg, RowsVi
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const float s = __uint_as_float(byte[j] << 23);
-    T* out = const_cast<T*>(row_of<T>(j ? v : k, token, head)) + 8 * c;
+    T* out = const_cast<T*>(row_at<T>(j ? v : k, token, head)) + 8 * c;
     if constexpr (std::is_same<T, float>::value) {
       const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 1),
                           __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[j], s, 3)};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *(f32x4_any*)(out + 4 * i) = f32x4_any{y[2 * i][0], y[2 * i][1], y[2 * i + 1][0], y[2 * i + 1][1]};
+      for (int i = 0; i < 2; ++i) *(f4_any*)(out + 4 * i) = f4_any{y[2 * i][0], y[2 * i][1], y[2 * i + 1][0], y[2 * i + 1][1]};
     } else {
-      u32x4 y;
+      w4 y;
       y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 0));
       y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 1));
       y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 2));
       y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s, 3));
-      *(u32x4*)out = y;
+      *(w4*)out = y;
     }
   }
 }

@@ -54,7 +54,6 @@ struct DealtArgs {
   int32_t groups;
 };
 
-__device__ __forceinline__ int32_t add_cap(int32_t x, int32_t y) { return min(x + y, kPagesCap); }
 // running sums over the workgroup, a thread's own left out, cut off at kPagesCap
 __device__ __forceinline__ int32_t scan(int32_t x, int32_t* all, int32_t* part) {
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;

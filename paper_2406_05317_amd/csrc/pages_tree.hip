@@ -120,8 +120,6 @@ __global__ __launch_bounds__(64 * kKeepWaves) void pages_keep_rows_k(PagesKeepAr
 // requests (saturating, as in the plan), a wave to a request that gives some.
 constexpr int kRingThreads = 1024;
 
-__device__ __forceinline__ int32_t add_cap(int32_t x, int32_t y) { return min(x + y, kPagesCap); }
-
 __global__ __launch_bounds__(kRingThreads) void pages_keep_ring_k(PagesKeepArgs a) {
   __shared__ int32_t off[kPagesMaxRequests], part[kRingThreads / 64], kept;
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;

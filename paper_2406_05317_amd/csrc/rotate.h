@@ -42,28 +42,8 @@ inline int32_t lanes_log(int32_t d) {
 
 namespace rotate_detail {
 
-typedef __attribute__((ext_vector_type(4))) uint32_t w4;
 typedef __attribute__((ext_vector_type(2))) uint32_t w2;
-typedef __attribute__((ext_vector_type(4), aligned(4))) float f4_any;          // fp32 rows begin at any float
 
-template <typename T>
-__device__ __forceinline__ void read8(const T* p, float (&x)[8]) {
-  if constexpr (std::is_same<T, float>::value) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f4_any v = *(const f4_any*)(p + 4 * i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
-    }
-  } else {
-    const w4 v = *(const w4*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(v[i] << 16);
-      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-  }
-}
 template <typename T>
 __device__ __forceinline__ void write8(T* p, const float (&x)[8]) {
   if constexpr (std::is_same<T, float>::value) {
@@ -75,12 +55,6 @@ __device__ __forceinline__ void write8(T* p, const float (&x)[8]) {
     for (int i = 0; i < 8; ++i) y[i] = (__bf16)x[i];
     *(w4*)p = *(const w4*)y;
   }
-}
-
-template <typename T>
-__device__ __forceinline__ const T* row_at(const RowsView& r, int32_t token, int32_t head) {
-  const int32_t b = token < r.t ? 0 : token / r.t, t = token - b * r.t;
-  return (const T*)r.p + b * r.sb + head * r.sh + t * r.st;
 }
 
 template <typename T>
