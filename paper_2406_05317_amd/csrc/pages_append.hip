@@ -36,7 +36,8 @@ __device__ __forceinline__ float off_border(float y, double x) {
 // not: it goes through LDS on the way.  A workgroup takes 2^lt positions and a block of q's, k's or v's heads, a lane's rows two at a time,
 // the next two on their way.  8186 prompt rows of 32 heads, bf16: 304 MB in 83 us (3.7 TB/s; a large copy 5.1), of it q alone 37, v 20, k 47: keys
 // wait for their chain of 64-bit arithmetic, LDS and conversion, with four waves to a SIMD by their registers (five spill: 181 us).  Keys' workgroups,
-// the longest, go first (92 us mixed with the others).  32 tokens: 5 us, three trips to memory and the functions of 64 bits.
+// the longest, go first (92 us mixed with the others).  With norm and weights 97 us; fp32 rows, 571 MB, 138 us and 144.  32 tokens: 5 us, three
+// trips to memory and the functions of 64 bits.
 template <typename T, int KIND>
 __global__ __launch_bounds__(kRotateThreads, KIND == kHalves ? 3 : 4) void pages_append_k(AppendArgs a) {
   __shared__ double2 table[kRotateTable];

@@ -28,10 +28,11 @@ __global__ __launch_bounds__(256) void pages_tree_join_k(TileArgs g, int32_t row
 // `per` is such that the parts of all long requests are about kParts: a request that is far longer than the others is cut into as many more.
 // Long ones go first, so that short ones fill up the end.  A tile in p parts has more than (p - 1) of their length: over all tiles in several
 // parts these are 2 kParts at most, and the tiles kParts at most.
-// 32 requests of 128 .. 8192 rows, trees of 8 .. 64, 8 kv heads of 4: 91 us against 100 dealt out as in lococo_pages_attn; one request of 131072
-// rows beside 31 of 500: 143 against 1033; 16 requests of up to 4000, 32 heads, where lengths are nearly even: 61 against 53.  The launch ahead takes
-// 7 us, the tiles what their vector instructions do: some 500 for 64 keys of 32 rows, beside 104 matrix products (some 1.2 us a step of a wave,
-// two of them on a SIMD); shorter parts add their starts, longer ones wait at the end (kAlone 16, kParts 1024: 84 us for 79).
+// 32 requests of 128 .. 8192 rows, trees of 8 .. 64, 8 kv heads of 4: 84 us a call against 94 dealt out as in lococo_pages_attn; 64 requests of 200
+// .. 8000 with 8 new rows 76 against 91; one request of 131072 rows beside 31 of 500: 145 against 1033.  Nearly even lengths, which the host cannot
+// tell, lose by it: 16 requests of up to 4000, 32 heads, 61 against 53; 8 of 8000 with 64 new rows 122 against 116.  The launch ahead takes
+// 7 - 8 us, the tiles (79 us of the 84) what their vector instructions do: some 500 for 64 keys of 32 rows, beside 104 matrix products (some 1.2 us a
+// step of a wave, two of them on a SIMD); shorter parts add their starts, longer ones wait at the end (kAlone 16, kParts 1024: 84 us for 79).
 constexpr int kAlone = 8, kParts = 512, kLeastSteps = 2, kDealThreads = 1024;
 constexpr int32_t kNoParts = kPagesCap / kTileKeys + 1;                      // steps of any request
 

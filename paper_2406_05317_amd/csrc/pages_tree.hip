@@ -76,7 +76,8 @@ __global__ void pages_tree_k(PagesTreeArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Keeping.  A wave to a request: the kept rows close up, in their order, on the places its new rows have had.
-// Bound by the launches: rows 2.7 us, ring 4 us for 32 requests and 10 for 256 (one workgroup: a running sum), moving 3.3 us.
+// Bound by the launches: rows 2.7 us, ring 4 us for 32 requests, 10.5 for 256 and 63 for 4096 (one workgroup, whose waves take the requests in turn),
+// moving 3.3 us.
 constexpr int kKeepWaves = 4;
 
 __global__ __launch_bounds__(64 * kKeepWaves) void pages_keep_rows_k(PagesKeepArgs a) {

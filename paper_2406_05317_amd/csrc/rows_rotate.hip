@@ -101,8 +101,8 @@ __global__ __launch_bounds__(kRotateThreads) void rows_rotate_k(RotateArgs a) {
 // Both means are sums over the row taken side by side.  A workgroup adds up its rows' part of d_w, once over its rows in LDS at the end, and
 // leaves it for rows_rotate_weights_k: no atomics, the same bits every time.  d_w is a sum over all rows of all heads: in fp32 over the eight
 // or fewer that a lane has of one tile (of eight tiles, where it has one of each), beyond them in 64 bits, a workgroup's part rounded to fp32.
-// In fp32 throughout it was twice as far from the exact sum.  Bound by memory: 16384 positions of 40 heads, 839 MB in 167 us (5.0 TB/s), the
-// weights' parts 8 more; with half as many workgroups 171, with a quarter 188.
+// In fp32 throughout it was twice as far from the exact sum.  Bound by memory: 16384 positions of 40 heads, 839 MB in 168 us (5.0 TB/s), the
+// weights' parts 9 more; with half as many workgroups 171, with a quarter 188.
 constexpr int kBackRows = 8;                   // rows whose part of d_w a lane adds up in fp32
 
 template <typename T, int KIND>
